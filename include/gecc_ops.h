@@ -1,0 +1,102 @@
+/*
+ * gecc_ops -- operators around a layer's products, for AMD MI355X (gfx950): microscaled 4-bit
+ * floating point (quantisation, products, the layer in training and serving) and the
+ * orthogonalised update of the layer's weight.  Part of libgecc; the conventions of gecc.h hold:
+ * 0-based indices, device buffers owned by the caller, everything enqueued on the stream handed in,
+ * no call synchronises or allocates, 0 or a negative GECC_ERR_* code comes back, nothing throws.
+ * The calls are stateless: they need no gecc_ctx, and calls that overlap in time need workspaces of
+ * their own.  None of them records a memset node, so all can be captured into a HIP graph.
+ *
+ * Microscaled 4-bit matrices ("mx4").  Every 32 consecutive values of a row share a power of two:
+ *   e = max(floor(log2(max |x|)) - 2, -127)  (-127 for a block of zeros),   value = q 2^e,
+ *   q = x 2^-e rounded to nearest, ties to the even code, in {0, .5, 1, 1.5, 2, 3, 4, 6}; beyond 6: 6.
+ * A block that holds a NaN or an infinity reads as NaN in all its places.  A matrix of `rows` rows of
+ * `cols` values is two buffers:
+ *   data    [rows][P / 2] bytes, P = cols rounded up to 256: two values a byte, the one of the lower
+ *           column in the lower half; a value is sign << 3 | code.  Columns from `cols` on hold 0.
+ *   scales  tiles of 16 rows x 16 blocks (512 columns), [ceil(rows / 16)][ceil(P / 512)] of them, 256
+ *           bytes each: [row % 16][block % 4][(block / 4) % 4], e + 127 in a byte, 255: NaN.  Places
+ *           beyond the matrix hold 0.  (The order in which the matrix instructions take them.)
+ * Both 16-byte aligned.  gecc_mx4_data_bytes / gecc_mx4_scale_bytes give the sizes.
+ */
+#ifndef GECC_OPS_H
+#define GECC_OPS_H
+
+#include "gecc.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+size_t gecc_mx4_data_bytes(int32_t rows, int32_t cols);
+size_t gecc_mx4_scale_bytes(int32_t rows, int32_t cols);
+
+/* X: rows x cols of dtype (GECC_F32 / GECC_BF16), row r at X + r * ld elements, ld >= cols; aligned to its
+   element (16-byte aligned rows take the vector path).
+   data, scales: X with blocks along its rows.  t_data, t_scales: the transpose of X (cols x rows, blocks along
+   the columns of X), as the products that contract the rows of X need it.  Either pair may be null; with both
+   X is read once. */
+int gecc_mx4_quantize(const void* dev_X, int32_t dtype, int32_t rows, int32_t cols, int64_t ld, void* dev_data,
+                      void* dev_scales, void* dev_t_data, void* dev_t_scales, void* stream);
+
+/* The values of an mx4 matrix as GECC_F32 or GECC_BF16 (exact in both), rows x cols at leading dimension ld. */
+int gecc_mx4_dequantize(const void* dev_data, const void* dev_scales, int32_t rows, int32_t cols, void* dev_out,
+                        int32_t dtype, int64_t ld, void* stream);
+
+/* C[n x m] = A[n x k] B[m x k]^T, both operands mx4 with k along the rows; sums in fp32, C of c_dtype at leading
+   dimension ldc >= m.  The workspace (gecc_mx4_gemm_workspace bytes, 256-byte aligned; may be null where that is 0)
+   holds partial sums of a product whose k is shared out. */
+size_t gecc_mx4_gemm_workspace(int32_t n, int32_t k, int32_t m);
+int gecc_mx4_gemm(int32_t n, int32_t k, int32_t m, const void* dev_A_data, const void* dev_A_scales,
+                  const void* dev_B_data, const void* dev_B_scales, void* dev_C, int32_t c_dtype, int64_t ldc,
+                  void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* The layer: Y[n x m] = Q(X[n x k]) W^T, W an mx4 matrix of m rows.  X (x_dtype, ldx >= k) is quantised on the way, bit
+   for bit as gecc_mx4_quantize does it: inside the product itself where it is small (a few tokens), else into the
+   workspace. */
+size_t gecc_mx4_linear_workspace(int32_t n, int32_t k, int32_t m);
+int gecc_mx4_linear(int32_t n, int32_t k, int32_t m, const void* dev_X, int32_t x_dtype, int64_t ldx,
+                    const void* dev_W_data, const void* dev_W_scales, void* dev_Y, int32_t y_dtype, int64_t ldy,
+                    void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* Its gradients (straight through the roundings): dX[n x k] = Q(dY) W, dW[m x k] = Q'(dY)^T X, with dY (n x m of dtype,
+   lddy >= m) quantised both ways in one pass; W_t: the transpose of W (k x m, blocks along the outputs), X_t: the
+   transpose of X (k x n, blocks along the tokens), both from gecc_mx4_quantize's transposed pair.  dX of dx_dtype at
+   lddx >= k, dW fp32 at lddw >= k; either may be null, and so may the operand it alone needs. */
+size_t gecc_mx4_linear_backward_workspace(int32_t n, int32_t k, int32_t m);
+int gecc_mx4_linear_backward(int32_t n, int32_t k, int32_t m, const void* dev_dY, int32_t dtype, int64_t lddy,
+                             const void* dev_Wt_data, const void* dev_Wt_scales, const void* dev_Xt_data,
+                             const void* dev_Xt_scales, void* dev_dX, int32_t dx_dtype, int64_t lddx, float* dev_dW,
+                             int64_t lddw, void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* The orthogonalised update of a weight, `batch` of them at once:
+     M <- mu M + G,  U = G + mu M (nesterov) or M;   without a momentum buffer U = G
+     X = U / (|U|_F + eps),  then `steps` times  X <- a X + (b S + c S S) X  with S = X X^T
+     O = scale X
+   on the shorter side (the transposes where rows > cols).  With coefficients like the default ones of the
+   binding the singular values of U are drawn towards 1 and its singular vectors stay.
+   X is held in 32 bits (two halves: 22 significant bits) up to the last step; S, its polynomial and the operand X of
+   the products in fp16 under powers of two that the coefficients fix; sums in fp32, the norm in fp64. */
+#define GECC_ORTH_MAX_STEPS 16
+typedef struct {
+  int32_t rows, cols, batch;      /* each >= 1                                                    */
+  int32_t dtype;                  /* of G: GECC_F32 or GECC_BF16                                  */
+  int32_t out_dtype;              /* of O: GECC_F32 or GECC_BF16                                  */
+  int32_t steps;                  /* 0 .. GECC_ORTH_MAX_STEPS                                     */
+  int32_t nesterov;               /* 0 / 1; read with a momentum buffer only                      */
+  int32_t reserved;               /* 0                                                            */
+  int64_t ld_g, ld_m, ld_o;       /* leading dimensions, >= cols                                  */
+  int64_t stride_g, stride_m, stride_o;   /* elements between batch items, >= rows * ld if batch > 1 */
+  float mu, eps, scale;           /* eps > 0                                                      */
+  float a, b, c;                  /* finite; refused (GECC_ERR_ARG) where they let a singular value
+                                     of X grow beyond 16 within `steps`                           */
+} gecc_orth_params;
+size_t gecc_orthogonalize_workspace(const gecc_orth_params* p);
+/* dev_G: read only.  dev_M: fp32, updated in place, or null.  dev_O: may not overlap the others. */
+int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_M, void* dev_O, void* dev_workspace,
+                       size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* GECC_OPS_H */

@@ -1,0 +1,384 @@
+// Microscaled 4-bit matrices: quantisation along rows, along columns, or both in one pass, the way back, and the product
+// with few rows (a serving step).  Layout and formulas: gecc_ops.h.
+//
+// All of it is bound by memory: bf16 in, 17/32 of a byte a value out for each direction.
+#include "ops_internal.h"
+#include "ops_device.h"
+
+namespace gecc {
+namespace {
+
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(8))) int i32x8_t;
+
+// scale byte of a block whose largest magnitude has these bits (an integer maximum: infinities and NaN are the largest)
+__device__ __forceinline__ unsigned scale_byte(unsigned amax) {
+  const int e = (int)(amax >> 23);
+  return e == 255 ? 255u : (unsigned)max(e - 2, 0);
+}
+// 2^-(byte - 127): between 2^-126 + 1 and 2^127, all normal (byte <= 252; of a NaN block: 0, so that its codes are 0)
+__device__ __forceinline__ float inverse_scale(unsigned byte) { return byte == 255 ? 0.f : __uint_as_float((254u - byte) << 23); }
+// 2^(byte - 127), byte 0: the subnormal 2^-127
+__device__ __forceinline__ float scale_value(unsigned byte) {
+  return byte == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float(byte == 0 ? 0x00400000u : byte << 23);
+}
+// eight values, already divided by the scale, to eight codes (round to nearest, ties to the even code, saturating)
+__device__ __forceinline__ unsigned pack8(const float (&v)[8]) {
+  unsigned r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0], v[1], 1.f, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2], v[3], 1.f, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4], v[5], 1.f, 2);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], 1.f, 3);
+  return r;
+}
+__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ float scaled(float x, float inv) { return inv == 0.f ? 0.f : x * inv; }
+
+// place of block `blk` of row `row` among the scales of a matrix with `units` tiles a row of tiles
+__device__ __forceinline__ int64_t scale_at(int64_t row, int64_t blk, int64_t units) {
+  return ((row >> 4) * units + (blk >> 4)) * 256 + (row & 15) * 16 + (blk & 3) * 4 + ((blk >> 2) & 3);
+}
+
+// maximum over groups of four neighbouring lanes
+__device__ __forceinline__ unsigned quad_max(unsigned x) {
+  x = max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0xb1, 0xf, 0xf, false));    // lanes 1 0 3 2
+  x = max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x4e, 0xf, 0xf, false));    // lanes 2 3 0 1
+  return x;
+}
+
+// Along the rows.  A workgroup takes one scale tile: 16 rows x 512 columns, a wavefront four of its rows, a lane eight
+// consecutive values of each, four lanes a block.
+template <bool F32, bool VEC>
+__global__ __launch_bounds__(256) void mx4_rows_kernel(MxQuantArgs a, int units) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int unit = blockIdx.x % units;
+  const int64_t row0 = (int64_t)(blockIdx.x / units) * 16 + wave * 4;
+  const int c = unit * MX_UNIT + lane * 8;
+  const int64_t pitch = mx_pad(a.cols) / 2;
+  float v[4][8];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) load8<F32, VEC>(a.X, (row0 + r) * a.ld + c, c, a.cols, row0 + r < a.rows, v[r]);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int64_t row = row0 + r;
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[r][i]));
+    const unsigned s = scale_byte(quad_max(m));
+    const float inv = inverse_scale(s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[r][i] = scaled(v[r][i], inv);
+    if (row < a.rows && c / 2 < pitch) *reinterpret_cast<unsigned*>(a.data + row * pitch + c / 2) = pack8(v[r]);
+    if ((lane & 3) == 0) a.scales[scale_at(row, c >> 5, units)] = (uint8_t)s;
+  }
+}
+
+// Along the columns, and along the rows with the same loads where BOTH.  A workgroup takes 128 rows x 256 bytes of
+// columns (128 bf16, 64 fp32) through LDS: rows as above (32 or 16 lanes a row), columns with a thread per block of 32
+// rows and one (fp32) or two (bf16) columns, whose LDS reads are 256 consecutive bytes a wavefront.
+template <bool F32, bool VEC, bool BOTH>
+__global__ __launch_bounds__(256) void mx4_cols_kernel(MxQuantArgs a, int col_tiles, int units, int t_units) {
+  constexpr int TR = 128, TC = F32 ? 64 : 128, LANES = TC / 8;      // lanes that hold a row
+  __shared__ __attribute__((aligned(16))) char tile[TR * 256];
+  const int tid = threadIdx.x;
+  const int c0 = (blockIdx.x % col_tiles) * TC;
+  const int64_t r0 = (int64_t)(blockIdx.x / col_tiles) * TR;
+  const int64_t pitch = mx_pad(a.cols) / 2, t_pitch = mx_pad(a.rows) / 2;
+  const int c = c0 + (tid % LANES) * 8;
+  constexpr int STEP = 256 / LANES, ITER = TR / STEP;
+  const int64_t rows16 = (a.rows + 15) / 16 * 16;
+#pragma unroll 1
+  for (int it0 = 0; it0 < ITER; it0 += 4) {
+    float v[4][8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t row = r0 + (it0 + q) * STEP + tid / LANES;
+      load8<F32, VEC>(a.X, row * a.ld + c, c, a.cols, row < a.rows, v[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int rr = (it0 + q) * STEP + tid / LANES;
+      const int64_t row = r0 + rr;
+      if (F32) {
+        f32x4_t* p = reinterpret_cast<f32x4_t*>(tile + rr * 256 + (tid % LANES) * 32);
+        p[0] = f32x4_t{v[q][0], v[q][1], v[q][2], v[q][3]};
+        p[1] = f32x4_t{v[q][4], v[q][5], v[q][6], v[q][7]};
+      } else {
+        u32x4_t w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (__float_as_uint(v[q][2 * i]) >> 16) | (__float_as_uint(v[q][2 * i + 1]) & 0xffff0000u);
+        *reinterpret_cast<u32x4_t*>(tile + rr * 256 + (tid % LANES) * 16) = w;
+      }
+      if (BOTH) {
+        unsigned m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[q][i]));
+        const unsigned s = scale_byte(quad_max(m));
+        const float inv = inverse_scale(s);
+        float u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = scaled(v[q][i], inv);
+        if (row < a.rows && c / 2 < pitch) *reinterpret_cast<unsigned*>(a.data + row * pitch + c / 2) = pack8(u);
+        if ((tid & 3) == 0 && row < rows16 && c < units * MX_UNIT) a.scales[scale_at(row, c >> 5, units)] = (uint8_t)s;
+      }
+    }
+  }
+  __syncthreads();
+  constexpr int NC = F32 ? 1 : 2;                  // columns of a thread
+  const int rb = tid >> 6, cc = (tid & 63) * NC;
+  float col[NC][32];
+#pragma unroll
+  for (int r = 0; r < 32; ++r) {
+    const unsigned w = *reinterpret_cast<const unsigned*>(tile + (rb * 32 + r) * 256 + (tid & 63) * 4);
+    if (F32) col[0][r] = __uint_as_float(w);
+    else { col[0][r] = __uint_as_float(w << 16); col[NC - 1][r] = __uint_as_float(w & 0xffff0000u); }
+  }
+  const int64_t row = r0 + rb * 32;
+  const int64_t cols16 = ((int64_t)a.cols + 15) / 16 * 16;
+#pragma unroll
+  for (int h = 0; h < NC; ++h) {
+    unsigned m = 0;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) m = max(m, magnitude(col[h][r]));
+    const unsigned s = scale_byte(m);
+    const float inv = inverse_scale(s);
+    u32x4_t w;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      float u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = scaled(col[h][8 * p + i], inv);
+      w[p] = pack8(u);
+    }
+    const int64_t cg = c0 + cc + h;
+    if (cg < a.cols && row / 2 < t_pitch) *reinterpret_cast<u32x4_t*>(a.t_data + cg * t_pitch + row / 2) = w;
+    if (cg < cols16 && row < (int64_t)t_units * MX_UNIT) a.t_scales[scale_at(cg, row >> 5, t_units)] = (uint8_t)s;
+  }
+}
+
+// The values again: a lane reads eight codes and their scale and writes eight values.
+template <bool F32, bool VEC>
+__global__ __launch_bounds__(256) void mx4_values_kernel(MxDequantArgs a, int units, int64_t chunks) {
+  const int64_t pitch = mx_pad(a.cols) / 2;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t per_row = (a.cols + 7) / 8;
+  if (id >= chunks) return;
+  const int64_t row = id / per_row;
+  const int c = (int)(id - row * per_row) * 8;
+  const unsigned w = *reinterpret_cast<const unsigned*>(a.data + row * pitch + c / 2);
+  const float s = scale_value(a.scales[scale_at(row, c >> 5, units)]);
+  float v[8];
+  const f32x2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1);
+  const f32x2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3);
+  v[0] = p0[0] * s; v[1] = p0[1] * s; v[2] = p1[0] * s; v[3] = p1[1] * s;
+  v[4] = p2[0] * s; v[5] = p2[1] * s; v[6] = p3[0] * s; v[7] = p3[1] * s;
+  if (F32) {
+    float* o = static_cast<float*>(a.out) + row * a.ld + c;
+    if (VEC && c + 8 <= a.cols) {
+      reinterpret_cast<f32x4_t*>(o)[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+      reinterpret_cast<f32x4_t*>(o)[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) if (c + i < a.cols) o[i] = v[i];
+    }
+  } else {
+    uint16_t* o = static_cast<uint16_t*>(a.out) + row * a.ld + c;
+    if (VEC && c + 8 <= a.cols) {
+      u32x4_t x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (unsigned)to_bf16(v[2 * i]) | ((unsigned)to_bf16(v[2 * i + 1]) << 16);
+      *reinterpret_cast<u32x4_t*>(o) = x;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) if (c + i < a.cols) o[i] = to_bf16(v[i]);
+    }
+  }
+}
+
+// Few rows of X: the weight is read once, everything else is small.  A workgroup takes 16 rows of W (a matrix
+// instruction's first operand: 16 rows x 128 columns, lane (r, g) holding the 32 columns of block g of row r) and up to
+// 16 NG rows of X as the second; its eight wavefronts share the units of 512 columns and add up through LDS, in order.
+// RAW: every workgroup quantises X itself, into LDS as [unit][step][group][lane] fragments.
+constexpr int FEW_WAVES = 8;
+constexpr int FEW_RAW_BYTES = 32768;      // packed X that a workgroup keeps
+
+template <int NG, bool RAW, bool F32X>
+__global__ __launch_bounds__(FEW_WAVES * 64) void mx4_few_kernel(MxFewArgs a, int units, bool vec_x, bool vec_y) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int l16 = lane & 15, g = lane >> 4;
+  const int64_t pitch = mx_pad(a.k) / 2;
+  const int steps = (int)(pitch / 64);                       // matrix instructions along k
+  const int w0 = blockIdx.x * 16;
+  const uint8_t* wrow = a.w_data + (int64_t)min(w0 + l16, a.m - 1) * pitch + g * 16;
+  const uint8_t* wsc = a.w_scales + ((int64_t)blockIdx.x * units) * 256 + l16 * 16 + g * 4;
+  char* xs = smem + FEW_WAVES * NG * 1024;                   // RAW: data [steps * n * 64], then scales [units * n * 16]
+  char* xsc = xs + (size_t)steps * a.n * 64;
+  if (RAW) {
+    // a lane quantises eight values; four lanes a block
+    const int per_row = steps * 16, total = a.n * per_row;       // chunks of eight columns
+    for (int o = tid; o < total; o += FEW_WAVES * 64) {     // (per_row is a multiple of 4: whole groups of lanes)
+      const int row = o / per_row, c = (o - row * per_row) * 8;
+      float v[8];
+      if (vec_x) load8<F32X, true>(a.x, (int64_t)row * a.ldx + c, c, a.k, true, v);
+      else load8<F32X, false>(a.x, (int64_t)row * a.ldx + c, c, a.k, true, v);
+      unsigned m = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+      const unsigned s = scale_byte(quad_max(m));
+      const float inv = inverse_scale(s);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = scaled(v[i], inv);
+      const int step = c >> 7, blk = (c >> 5) & 3;
+      *reinterpret_cast<unsigned*>(xs + ((step * a.n + row) * 4 + blk) * 16 + ((c >> 3) & 3) * 4) = pack8(v);
+      if ((o & 3) == 0) xsc[(((step >> 2) * a.n + row) * 4 + blk) * 4 + (step & 3)] = (char)s;
+    }
+    __syncthreads();
+  }
+  f32x4_t acc[NG];
+#pragma unroll
+  for (int q = 0; q < NG; ++q) acc[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int u = wave; u < units; u += FEW_WAVES) {
+    u32x4_t w[4], x[NG][4];
+    int ws, sx[NG];
+    const int left = steps - 4 * u;          // 4, or 2 in a last half unit
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      w[j] = j < left ? *reinterpret_cast<const u32x4_t*>(wrow + (int64_t)(4 * u + j) * 64) : u32x4_t{0, 0, 0, 0};
+    ws = *reinterpret_cast<const int*>(wsc + (int64_t)u * 256);
+#pragma unroll
+    for (int q = 0; q < NG; ++q) {
+      const int row = q * 16 + l16;
+      const bool ok = row < a.n;
+      sx[q] = 0;
+      if (ok) sx[q] = RAW ? *reinterpret_cast<const int*>(xsc + ((u * a.n + row) * 4 + g) * 4)
+                          : *reinterpret_cast<const int*>(a.x_scales + ((int64_t)q * units + u) * 256 + l16 * 16 + g * 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[q][j] = u32x4_t{0, 0, 0, 0};
+        if (ok && j < left)
+          x[q][j] = RAW ? *reinterpret_cast<const u32x4_t*>(xs + (((4 * u + j) * a.n + row) * 4 + g) * 16)
+                        : *reinterpret_cast<const u32x4_t*>(a.x_data + (int64_t)row * pitch + (4 * u + j) * 64 + g * 16);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < NG; ++q) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (j >= left) break;                // (there are no scales either)
+        const i32x8_t fa = {(int)w[j][0], (int)w[j][1], (int)w[j][2], (int)w[j][3], 0, 0, 0, 0};
+        const i32x8_t fb = {(int)x[q][j][0], (int)x[q][j][1], (int)x[q][j][2], (int)x[q][j][3], 0, 0, 0, 0};
+        // (the byte of the scale registers is a constant of the instruction)
+        if (j == 0) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 0, ws, 0, sx[q]);
+        if (j == 1) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 1, ws, 1, sx[q]);
+        if (j == 2) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 2, ws, 2, sx[q]);
+        if (j == 3) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 3, ws, 3, sx[q]);
+      }
+    }
+  }
+  f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);
+#pragma unroll
+  for (int q = 0; q < NG; ++q) red[(wave * NG + q) * 64 + lane] = acc[q];
+  __syncthreads();
+  if (wave < NG) {
+    f32x4_t s = red[wave * 64 + lane];
+#pragma unroll
+    for (int w = 1; w < FEW_WAVES; ++w) {
+      const f32x4_t t = red[(w * NG + wave) * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] += t[i];
+    }
+    const int row = wave * 16 + l16, col = w0 + 4 * g;
+    if (row < a.n) {
+      if (a.y_dtype == GECC_F32) {
+        float* y = static_cast<float*>(a.y) + (int64_t)row * a.ldy + col;
+        if (vec_y && col + 4 <= a.m) *reinterpret_cast<f32x4_t*>(y) = s;
+        else
+          for (int i = 0; i < 4; ++i) if (col + i < a.m) y[i] = s[i];
+      } else {
+        uint16_t* y = static_cast<uint16_t*>(a.y) + (int64_t)row * a.ldy + col;
+        if (vec_y && col + 4 <= a.m)
+          *reinterpret_cast<u32x2_t*>(y) = u32x2_t{(unsigned)to_bf16(s[0]) | ((unsigned)to_bf16(s[1]) << 16),
+                                                   (unsigned)to_bf16(s[2]) | ((unsigned)to_bf16(s[3]) << 16)};
+        else
+          for (int i = 0; i < 4; ++i) if (col + i < a.m) y[i] = to_bf16(s[i]);
+      }
+    }
+  }
+}
+
+template <int NG>
+hipError_t few(const MxFewArgs& a, int units, hipStream_t st) {
+  const int64_t es = a.x_dtype == GECC_F32 ? 4 : 2, ey = a.y_dtype == GECC_F32 ? 4 : 2;
+  const bool vec_x = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * es % 16 == 0;
+  const bool vec_y = reinterpret_cast<uintptr_t>(a.y) % (4 * ey) == 0 && a.ldy % 4 == 0;
+  const dim3 grid((a.m + 15) / 16), block(FEW_WAVES * 64);
+  size_t lds = FEW_WAVES * NG * 1024;
+  if (a.x) {
+    lds += (size_t)a.n * mx_pad(a.k) / 2 + (size_t)a.n * units * 16;
+    if (a.x_dtype == GECC_F32) hipLaunchKernelGGL((mx4_few_kernel<NG, true, true>), grid, block, lds, st, a, units, vec_x, vec_y);
+    else hipLaunchKernelGGL((mx4_few_kernel<NG, true, false>), grid, block, lds, st, a, units, vec_x, vec_y);
+  } else {
+    hipLaunchKernelGGL((mx4_few_kernel<NG, false, false>), grid, block, lds, st, a, units, vec_x, vec_y);
+  }
+  return hipGetLastError();
+}
+
+template <bool F32, bool VEC>
+hipError_t quantize(const MxQuantArgs& a, hipStream_t st) {
+  const int64_t units = mx_units(a.cols), t_units = mx_units(a.rows);
+  if (!a.t_data) {
+    const int64_t grid = units * ((a.rows + 15) / 16);
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((mx4_rows_kernel<F32, VEC>), dim3((unsigned)grid), dim3(256), 0, st, a, (int)units);
+    return hipGetLastError();
+  }
+  // (tiles cover the padding of the scales: 512 columns each way)
+  constexpr int TC = F32 ? 64 : 128;
+  const int64_t col_tiles = a.data ? units * MX_UNIT / TC : ((a.cols + 15) / 16 * 16 + TC - 1) / TC;
+  const int64_t grid = col_tiles * (t_units * MX_UNIT / 128);
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  if (a.data) hipLaunchKernelGGL((mx4_cols_kernel<F32, VEC, true>), dim3((unsigned)grid), dim3(256), 0, st, a, (int)col_tiles, (int)units, (int)t_units);
+  else hipLaunchKernelGGL((mx4_cols_kernel<F32, VEC, false>), dim3((unsigned)grid), dim3(256), 0, st, a, (int)col_tiles, (int)units, (int)t_units);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_mx4_quantize(const MxQuantArgs& a, hipStream_t st) {
+  const int64_t es = a.dtype == GECC_F32 ? 4 : 2;
+  const bool vec = reinterpret_cast<uintptr_t>(a.X) % 16 == 0 && a.ld * es % 16 == 0;
+  if (a.dtype == GECC_F32) return vec ? quantize<true, true>(a, st) : quantize<true, false>(a, st);
+  return vec ? quantize<false, true>(a, st) : quantize<false, false>(a, st);
+}
+
+hipError_t launch_mx4_dequantize(const MxDequantArgs& a, hipStream_t st) {
+  const int64_t es = a.dtype == GECC_F32 ? 4 : 2;
+  const bool vec = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.ld * es % 16 == 0;
+  const int64_t chunks = (int64_t)a.rows * ((a.cols + 7) / 8), grid = (chunks + 255) / 256;
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  const int units = (int)mx_units(a.cols);
+  const dim3 g((unsigned)grid), b(256);
+  if (a.dtype == GECC_F32) {
+    if (vec) hipLaunchKernelGGL((mx4_values_kernel<true, true>), g, b, 0, st, a, units, chunks);
+    else hipLaunchKernelGGL((mx4_values_kernel<true, false>), g, b, 0, st, a, units, chunks);
+  } else {
+    if (vec) hipLaunchKernelGGL((mx4_values_kernel<false, true>), g, b, 0, st, a, units, chunks);
+    else hipLaunchKernelGGL((mx4_values_kernel<false, false>), g, b, 0, st, a, units, chunks);
+  }
+  return hipGetLastError();
+}
+
+bool mx4_few_raw_ok(int n, int k) {
+  return n <= MX_FEW_ROWS && (int64_t)n * (mx_pad(k) / 2 + mx_units(k) * 16) <= FEW_RAW_BYTES;
+}
+
+hipError_t launch_mx4_few(const MxFewArgs& a, hipStream_t st) {
+  if (a.n < 1 || a.n > MX_FEW_ROWS || (a.x && !mx4_few_raw_ok(a.n, a.k))) return hipErrorInvalidValue;
+  const int units = (int)mx_units(a.k);
+  if (a.n <= 16) return few<1>(a, units, st);
+  if (a.n <= 32) return few<2>(a, units, st);
+  return few<4>(a, units, st);
+}
+
+}  // namespace gecc

@@ -1,0 +1,367 @@
+// C ABI of the operators of gecc_ops.h: argument checking, workspace layout and launch sequences.  Host code only.
+#include <cmath>
+#include "ops_internal.h"
+
+using namespace gecc;
+
+namespace {
+
+constexpr int32_t MAX_SIDE = 1 << 24;      // rows and columns: byte offsets inside a tile then fit 32 bits
+
+size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+bool side_ok(int32_t v) { return v >= 1 && v <= MAX_SIDE; }
+bool dtype_ok(int32_t d) { return d == GECC_F32 || d == GECC_BF16; }
+size_t elem_size(int32_t d) { return d == GECC_BF16 ? 2 : 4; }
+int hip_rc(hipError_t e) { return e == hipSuccess ? GECC_OK : GECC_ERR_HIP; }
+int check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return GECC_OK;
+  if (!ws) return GECC_ERR_WORKSPACE;
+  if (!aligned_to(ws, 256)) return GECC_ERR_ALIGN;
+  return bytes < need ? GECC_ERR_WORKSPACE : GECC_OK;
+}
+
+size_t data_bytes(int64_t rows, int64_t cols) { return (size_t)rows * (mx_pad(cols) / 2); }
+size_t scale_bytes(int64_t rows, int64_t cols) { return (size_t)((rows + 15) / 16) * mx_units(cols) * 256; }
+
+int mx_stages(int64_t k) { return (int)(mx_pad(k) / MX_PAD); }
+
+// ---- C[n x m] = A[n x k] B[m x k]^T ------------------------------------------------------------------
+TilePlan product_plan(int32_t n, int32_t k, int32_t m) {
+  return plan_tiles(KIND_MX4, EPI_OUT, m, n, mx_stages(k), 1, false);
+}
+size_t product_workspace(int32_t n, int32_t k, int32_t m) {
+  return n <= MX_FEW_ROWS ? 0 : align_up(product_plan(n, k, m).part_bytes, 256);
+}
+hipError_t product(int32_t n, int32_t k, int32_t m, const uint8_t* a_data, const uint8_t* a_scales, const uint8_t* b_data,
+                   const uint8_t* b_scales, void* C, int32_t c_dtype, int64_t ldc, void* ws, hipStream_t st) {
+  if (n <= MX_FEW_ROWS) {
+    MxFewArgs f{};
+    f.n = n; f.k = k; f.m = m;
+    f.x_data = a_data; f.x_scales = a_scales; f.w_data = b_data; f.w_scales = b_scales;
+    f.y = C; f.y_dtype = c_dtype; f.ldy = ldc;
+    return launch_mx4_few(f, st);
+  }
+  TileArgs t{};
+  // (the stored side of a lane's four values is the tile's first operand: the columns of C)
+  t.A = b_data; t.B = a_data;
+  t.lda = t.ldb = mx_pad(k) / 2;
+  t.scale_a = b_scales; t.scale_b = a_scales;
+  t.m_rows = m; t.n_rows = n;
+  t.stages = mx_stages(k);
+  t.batch = 1;
+  t.part = static_cast<float*>(ws);
+  t.out = C; t.ldo = ldc; t.out_dtype = c_dtype;
+  return launch_tiles(KIND_MX4, EPI_OUT, t, product_plan(n, k, m), st);
+}
+
+struct LinearLayout { size_t x_data, x_scales, part, total; bool raw; };
+LinearLayout linear_layout(int32_t n, int32_t k, int32_t m) {
+  LinearLayout l{};
+  l.raw = mx4_few_raw_ok(n, k);
+  if (l.raw) return l;
+  l.x_scales = align_up(data_bytes(n, k), 256);
+  l.part = l.x_scales + align_up(scale_bytes(n, k), 256);
+  l.total = l.part + product_workspace(n, k, m);
+  return l;
+}
+
+struct BackwardLayout { size_t q_scales, t_data, t_scales, part, total; };
+BackwardLayout backward_layout(int32_t n, int32_t k, int32_t m) {
+  BackwardLayout l{};
+  l.q_scales = align_up(data_bytes(n, m), 256);
+  l.t_data = l.q_scales + align_up(scale_bytes(n, m), 256);
+  l.t_scales = l.t_data + align_up(data_bytes(m, n), 256);
+  l.part = l.t_scales + align_up(scale_bytes(m, n), 256);
+  const size_t dx = product_workspace(n, m, k), dw = product_workspace(m, n, k);
+  l.total = l.part + (dx > dw ? dx : dw);
+  return l;
+}
+
+// ---- the orthogonalised update ------------------------------------------------------------------------
+struct OrthPlan {
+  int s, l;
+  bool tall;
+  int64_t sp, lp;                 // padded to 64
+  int nparts;
+  TilePlan gram, poly, update;
+  size_t parts, x[2], lo[2], gram_at, poly_at, part, total;
+  float sx[GECC_ORTH_MAX_STEPS + 1], ss[GECC_ORTH_MAX_STEPS], sp_[GECC_ORTH_MAX_STEPS];    // powers of two that X, S, P are stored with
+};
+
+// a power of two that brings values up to `most` to at most half of fp16's range
+float power_for(double most) {
+  if (most < 0x1p-10) most = 0x1p-10;
+  return (float)std::ldexp(1.0, (int)std::floor(std::log2(32768.0 / most)));
+}
+
+// X has no singular value above 1 (its Frobenius norm is at most 1), and a step maps each by a polynomial: the largest
+// value of the polynomials over what is reached bounds every element of X, S and P, whatever the data.
+bool orth_scales(const gecc_orth_params& p, OrthPlan* o) {
+  double sig = 1.0;
+  for (int t = 0; t < p.steps; ++t) {
+    sig *= 1.0 + 0x1p-6;          // rounding, and maxima between the points
+    o->sx[t] = power_for(sig);
+    o->ss[t] = power_for(sig * sig);
+    double next = 0.0, poly = 0.0;
+    for (int i = 0; i <= 2048; ++i) {
+      const double x = sig * i / 2048, y = x * x, q = (double)p.b * y + (double)p.c * y * y;
+      poly = std::fmax(poly, std::fabs(q));
+      next = std::fmax(next, std::fabs(x * ((double)p.a + q)));
+    }
+    o->sp_[t] = power_for(poly * (1.0 + 0x1p-6));
+    if (!(next <= 16.0) || !(poly <= 4096.0)) return false;
+    sig = next;
+  }
+  o->sx[p.steps] = 1.f;
+  return true;
+}
+
+bool orth_plan(const gecc_orth_params* p, OrthPlan* o) {
+  if (!p || !side_ok(p->rows) || !side_ok(p->cols) || p->batch < 1 || p->batch > 65535) return false;
+  if (!dtype_ok(p->dtype) || !dtype_ok(p->out_dtype) || p->reserved != 0) return false;
+  if (p->steps < 0 || p->steps > GECC_ORTH_MAX_STEPS || (p->nesterov != 0 && p->nesterov != 1)) return false;
+  if (!std::isfinite(p->mu) || !std::isfinite(p->scale) || !(p->eps > 0) || !std::isfinite(p->eps)) return false;
+  if (!std::isfinite(p->a) || !std::isfinite(p->b) || !std::isfinite(p->c)) return false;
+  if (!orth_scales(*p, o)) return false;
+  o->tall = p->rows > p->cols;
+  o->s = o->tall ? p->cols : p->rows;
+  o->l = o->tall ? p->rows : p->cols;
+  o->sp = align_up(o->s, 64);
+  o->lp = align_up(o->l, 64);
+  const int64_t elements = (int64_t)p->rows * p->cols;
+  int64_t parts = (elements + 8191) / 8192;
+  // (256 workgroups in all are few, a partial sum for each of them at every start of the next pass is not)
+  o->nparts = (int)(parts > ORTH_PARTS ? ORTH_PARTS : parts);
+  o->gram = plan_tiles(KIND_F16, EPI_GRAM, o->s, o->s, (int)(o->lp / 64), p->batch, true);
+  o->poly = plan_tiles(KIND_F16, EPI_POLY, o->s, o->s, (int)(o->sp / 64), p->batch, true);
+  o->update = plan_tiles(KIND_F16, EPI_UPDATE, o->l, o->s, (int)(o->sp / 64), p->batch, false);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
+  const size_t x = (size_t)p->batch * o->s * o->lp * 2, q = (size_t)p->batch * o->s * o->sp * 2;
+  o->parts = take((size_t)p->batch * o->nparts * sizeof(double));
+  if (p->steps > 0) {
+    o->x[0] = take(x); o->lo[0] = take(x); o->x[1] = take(x); o->lo[1] = take(x);
+    o->gram_at = take(q);
+    o->poly_at = take(q);
+    size_t part = o->gram.part_bytes;
+    if (o->poly.part_bytes > part) part = o->poly.part_bytes;
+    if (o->update.part_bytes > part) part = o->update.part_bytes;
+    o->part = take(part);
+  }
+  o->total = off;
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t gecc_mx4_data_bytes(int32_t rows, int32_t cols) { return side_ok(rows) && side_ok(cols) ? data_bytes(rows, cols) : 0; }
+size_t gecc_mx4_scale_bytes(int32_t rows, int32_t cols) { return side_ok(rows) && side_ok(cols) ? scale_bytes(rows, cols) : 0; }
+
+int gecc_mx4_quantize(const void* dev_X, int32_t dtype, int32_t rows, int32_t cols, int64_t ld, void* dev_data,
+                      void* dev_scales, void* dev_t_data, void* dev_t_scales, void* stream) {
+  if (!dev_X || !dtype_ok(dtype) || !side_ok(rows) || !side_ok(cols) || ld < cols) return GECC_ERR_ARG;
+  if (!dev_data != !dev_scales || !dev_t_data != !dev_t_scales || (!dev_data && !dev_t_data)) return GECC_ERR_ARG;
+  if (!aligned_to(dev_X, elem_size(dtype)) || !aligned_to(dev_data, 16) || !aligned_to(dev_scales, 16) ||
+      !aligned_to(dev_t_data, 16) || !aligned_to(dev_t_scales, 16))
+    return GECC_ERR_ALIGN;
+  const MxQuantArgs a = {dev_X, dtype, rows, cols, ld, static_cast<uint8_t*>(dev_data), static_cast<uint8_t*>(dev_scales),
+                         static_cast<uint8_t*>(dev_t_data), static_cast<uint8_t*>(dev_t_scales)};
+  return hip_rc(launch_mx4_quantize(a, (hipStream_t)stream));
+}
+
+int gecc_mx4_dequantize(const void* dev_data, const void* dev_scales, int32_t rows, int32_t cols, void* dev_out,
+                        int32_t dtype, int64_t ld, void* stream) {
+  if (!dev_data || !dev_scales || !dev_out || !dtype_ok(dtype) || !side_ok(rows) || !side_ok(cols) || ld < cols) return GECC_ERR_ARG;
+  if (!aligned_to(dev_data, 16) || !aligned_to(dev_scales, 16) || !aligned_to(dev_out, elem_size(dtype))) return GECC_ERR_ALIGN;
+  const MxDequantArgs a = {static_cast<const uint8_t*>(dev_data), static_cast<const uint8_t*>(dev_scales), dev_out, dtype, rows, cols, ld};
+  return hip_rc(launch_mx4_dequantize(a, (hipStream_t)stream));
+}
+
+size_t gecc_mx4_gemm_workspace(int32_t n, int32_t k, int32_t m) {
+  return side_ok(n) && side_ok(k) && side_ok(m) ? product_workspace(n, k, m) : 0;
+}
+
+int gecc_mx4_gemm(int32_t n, int32_t k, int32_t m, const void* dev_A_data, const void* dev_A_scales,
+                  const void* dev_B_data, const void* dev_B_scales, void* dev_C, int32_t c_dtype, int64_t ldc,
+                  void* dev_workspace, size_t workspace_bytes, void* stream) {
+  if (!side_ok(n) || !side_ok(k) || !side_ok(m) || !dtype_ok(c_dtype) || ldc < m) return GECC_ERR_ARG;
+  if (!dev_A_data || !dev_A_scales || !dev_B_data || !dev_B_scales || !dev_C) return GECC_ERR_ARG;
+  if (!aligned_to(dev_A_data, 16) || !aligned_to(dev_A_scales, 16) || !aligned_to(dev_B_data, 16) ||
+      !aligned_to(dev_B_scales, 16) || !aligned_to(dev_C, elem_size(c_dtype)))
+    return GECC_ERR_ALIGN;
+  const int rc = check_workspace(dev_workspace, workspace_bytes, product_workspace(n, k, m));
+  if (rc) return rc;
+  return hip_rc(product(n, k, m, static_cast<const uint8_t*>(dev_A_data), static_cast<const uint8_t*>(dev_A_scales),
+                        static_cast<const uint8_t*>(dev_B_data), static_cast<const uint8_t*>(dev_B_scales), dev_C, c_dtype, ldc,
+                        dev_workspace, (hipStream_t)stream));
+}
+
+size_t gecc_mx4_linear_workspace(int32_t n, int32_t k, int32_t m) {
+  return side_ok(n) && side_ok(k) && side_ok(m) ? linear_layout(n, k, m).total : 0;
+}
+
+int gecc_mx4_linear(int32_t n, int32_t k, int32_t m, const void* dev_X, int32_t x_dtype, int64_t ldx,
+                    const void* dev_W_data, const void* dev_W_scales, void* dev_Y, int32_t y_dtype, int64_t ldy,
+                    void* dev_workspace, size_t workspace_bytes, void* stream) {
+  if (!side_ok(n) || !side_ok(k) || !side_ok(m) || !dtype_ok(x_dtype) || !dtype_ok(y_dtype) || ldx < k || ldy < m) return GECC_ERR_ARG;
+  if (!dev_X || !dev_W_data || !dev_W_scales || !dev_Y) return GECC_ERR_ARG;
+  if (!aligned_to(dev_X, elem_size(x_dtype)) || !aligned_to(dev_W_data, 16) || !aligned_to(dev_W_scales, 16) ||
+      !aligned_to(dev_Y, elem_size(y_dtype)))
+    return GECC_ERR_ALIGN;
+  const LinearLayout l = linear_layout(n, k, m);
+  const int rc = check_workspace(dev_workspace, workspace_bytes, l.total);
+  if (rc) return rc;
+  const hipStream_t st = (hipStream_t)stream;
+  const uint8_t* w_data = static_cast<const uint8_t*>(dev_W_data);
+  const uint8_t* w_scales = static_cast<const uint8_t*>(dev_W_scales);
+  if (l.raw) {
+    MxFewArgs f{};
+    f.n = n; f.k = k; f.m = m;
+    f.x = dev_X; f.x_dtype = x_dtype; f.ldx = ldx;
+    f.w_data = w_data; f.w_scales = w_scales;
+    f.y = dev_Y; f.y_dtype = y_dtype; f.ldy = ldy;
+    return hip_rc(launch_mx4_few(f, st));
+  }
+  uint8_t* ws = static_cast<uint8_t*>(dev_workspace);
+  const MxQuantArgs q = {dev_X, x_dtype, n, k, ldx, ws + l.x_data, ws + l.x_scales, nullptr, nullptr};
+  const hipError_t e = launch_mx4_quantize(q, st);
+  if (e != hipSuccess) return hip_rc(e);
+  return hip_rc(product(n, k, m, ws + l.x_data, ws + l.x_scales, w_data, w_scales, dev_Y, y_dtype, ldy, ws + l.part, st));
+}
+
+size_t gecc_mx4_linear_backward_workspace(int32_t n, int32_t k, int32_t m) {
+  return side_ok(n) && side_ok(k) && side_ok(m) ? backward_layout(n, k, m).total : 0;
+}
+
+int gecc_mx4_linear_backward(int32_t n, int32_t k, int32_t m, const void* dev_dY, int32_t dtype, int64_t lddy,
+                             const void* dev_Wt_data, const void* dev_Wt_scales, const void* dev_Xt_data,
+                             const void* dev_Xt_scales, void* dev_dX, int32_t dx_dtype, int64_t lddx, float* dev_dW,
+                             int64_t lddw, void* dev_workspace, size_t workspace_bytes, void* stream) {
+  if (!side_ok(n) || !side_ok(k) || !side_ok(m) || !dtype_ok(dtype) || !dev_dY || lddy < m || (!dev_dX && !dev_dW)) return GECC_ERR_ARG;
+  if (dev_dX && (!dev_Wt_data || !dev_Wt_scales || !dtype_ok(dx_dtype) || lddx < k)) return GECC_ERR_ARG;
+  if (dev_dW && (!dev_Xt_data || !dev_Xt_scales || lddw < k)) return GECC_ERR_ARG;
+  if (!aligned_to(dev_dY, elem_size(dtype)) || (dev_dX && !aligned_to(dev_dX, elem_size(dx_dtype))) || !aligned_to(dev_dW, 4) ||
+      !aligned_to(dev_Wt_data, 16) || !aligned_to(dev_Wt_scales, 16) || !aligned_to(dev_Xt_data, 16) || !aligned_to(dev_Xt_scales, 16))
+    return GECC_ERR_ALIGN;
+  const BackwardLayout l = backward_layout(n, k, m);
+  const int rc = check_workspace(dev_workspace, workspace_bytes, l.total);
+  if (rc) return rc;
+  const hipStream_t st = (hipStream_t)stream;
+  uint8_t* ws = static_cast<uint8_t*>(dev_workspace);
+  MxQuantArgs q = {dev_dY, dtype, n, m, lddy, nullptr, nullptr, nullptr, nullptr};
+  if (dev_dX) { q.data = ws; q.scales = ws + l.q_scales; }
+  if (dev_dW) { q.t_data = ws + l.t_data; q.t_scales = ws + l.t_scales; }
+  hipError_t e = launch_mx4_quantize(q, st);
+  if (e == hipSuccess && dev_dX)
+    e = product(n, m, k, ws, ws + l.q_scales, static_cast<const uint8_t*>(dev_Wt_data), static_cast<const uint8_t*>(dev_Wt_scales), dev_dX,
+                dx_dtype, lddx, ws + l.part, st);
+  if (e == hipSuccess && dev_dW)
+    e = product(m, n, k, ws + l.t_data, ws + l.t_scales, static_cast<const uint8_t*>(dev_Xt_data), static_cast<const uint8_t*>(dev_Xt_scales),
+                dev_dW, GECC_F32, lddw, ws + l.part, st);
+  return hip_rc(e);
+}
+
+size_t gecc_orthogonalize_workspace(const gecc_orth_params* p) {
+  OrthPlan o;
+  return orth_plan(p, &o) ? o.total : 0;
+}
+
+int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_M, void* dev_O, void* dev_workspace,
+                       size_t workspace_bytes, void* stream) {
+  OrthPlan o;
+  if (!orth_plan(p, &o) || !dev_G || !dev_O) return GECC_ERR_ARG;
+  if (p->ld_g < p->cols || p->ld_o < p->cols || (dev_M && p->ld_m < p->cols)) return GECC_ERR_ARG;
+  if (p->batch > 1 && (p->stride_g < p->rows * p->ld_g || p->stride_o < p->rows * p->ld_o || (dev_M && p->stride_m < p->rows * p->ld_m)))
+    return GECC_ERR_ARG;
+  if (!aligned_to(dev_G, elem_size(p->dtype)) || !aligned_to(dev_M, 4) || !aligned_to(dev_O, elem_size(p->out_dtype))) return GECC_ERR_ALIGN;
+  const int rc = check_workspace(dev_workspace, workspace_bytes, o.total);
+  if (rc) return rc;
+  const hipStream_t st = (hipStream_t)stream;
+  char* ws = static_cast<char*>(dev_workspace);
+  auto half = [&](size_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
+
+  OrthPrepArgs prep{};
+  prep.p = *p;
+  prep.G = dev_G;
+  prep.M = dev_M;
+  prep.parts = reinterpret_cast<double*>(ws + o.parts);
+  prep.nparts = o.nparts;
+  prep.s = o.s; prep.l = o.l; prep.lp = o.lp; prep.tall = o.tall;
+  prep.x_scale = o.sx[0];
+  hipError_t e = launch_orth_norm(prep, st);
+  if (e != hipSuccess) return hip_rc(e);
+  if (p->steps == 0) return hip_rc(launch_orth_store(prep, dev_O, st));
+  prep.hi = half(o.x[0]);
+  prep.lo = half(o.lo[0]);
+  e = launch_orth_start(prep, st);
+
+  const int64_t xs = (int64_t)o.s * o.lp, qs = (int64_t)o.s * o.sp;     // elements of X, of S and P
+  for (int t = 0; t < p->steps && e == hipSuccess; ++t) {
+    const int cur = t & 1;
+    const bool last = t + 1 == p->steps;
+    const float sx = o.sx[t], ss = o.ss[t], sp = o.sp_[t];
+    TileArgs g{};
+    g.A = g.B = reinterpret_cast<const uint8_t*>(half(o.x[cur]));
+    g.lda = g.ldb = o.lp * 2;
+    g.sa = g.sb = xs * 2;
+    g.m_rows = g.n_rows = o.s;
+    g.stages = (int)(o.lp / 64);
+    g.batch = p->batch;
+    g.part = reinterpret_cast<float*>(ws + o.part);
+    g.symmetric = true;
+    g.out = half(o.gram_at);
+    g.ldo = o.sp; g.so = qs;
+    g.m_store = (int)o.sp; g.n_store = o.s;
+    g.f_acc = ss / (sx * sx);
+    e = launch_tiles(KIND_F16, EPI_GRAM, g, o.gram, st);
+    if (e != hipSuccess) break;
+    TileArgs q = g;
+    q.A = q.B = reinterpret_cast<const uint8_t*>(half(o.gram_at));
+    q.lda = q.ldb = o.sp * 2;
+    q.sa = q.sb = qs * 2;
+    q.stages = (int)(o.sp / 64);
+    q.out = half(o.poly_at);
+    q.old_hi = half(o.gram_at);
+    q.ld_old = o.sp; q.s_old = qs;
+    q.f_old = (float)((double)p->b * sp / ss);
+    q.f_acc = (float)((double)p->c * sp / ((double)ss * ss));
+    e = launch_tiles(KIND_F16, EPI_POLY, q, o.poly, st);
+    if (e != hipSuccess) break;
+    TileArgs u{};
+    u.A = reinterpret_cast<const uint8_t*>(half(o.x[cur]));
+    u.lda = o.lp * 2; u.sa = xs * 2;
+    u.a_cols = (int)o.lp; u.k_rows = o.s;
+    u.B = reinterpret_cast<const uint8_t*>(half(o.poly_at));
+    u.ldb = o.sp * 2; u.sb = qs * 2;
+    u.m_rows = o.l; u.n_rows = o.s;
+    u.stages = (int)(o.sp / 64);
+    u.batch = p->batch;
+    u.part = g.part;
+    u.old_hi = half(o.x[cur]);
+    // (the last step's X is in one half: nothing grows what its rounding adds any more)
+    u.old_lo = t == 0 || !last ? half(o.lo[cur]) : nullptr;
+    u.ld_old = o.lp; u.s_old = xs;
+    u.m_store = (int)o.lp; u.n_store = o.s;
+    u.last = last;
+    const double to = last ? (double)p->scale : (double)o.sx[t + 1];
+    u.f_old = (float)(to * p->a / sx);
+    u.f_acc = (float)(to / ((double)sp * sx));
+    if (last) {
+      u.out = dev_O;
+      u.ldo = p->ld_o; u.so = p->batch > 1 ? p->stride_o : 0;
+      u.out_dtype = p->out_dtype;
+      u.transpose_out = o.tall;
+    } else {
+      u.out = half(o.x[cur ^ 1]);
+      u.ldo = o.lp; u.so = xs;
+      u.out_lo = t + 2 < p->steps ? half(o.lo[cur ^ 1]) : nullptr;
+    }
+    e = launch_tiles(KIND_F16, EPI_UPDATE, u, o.update, st);
+  }
+  return hip_rc(e);
+}
+
+}  // extern "C"

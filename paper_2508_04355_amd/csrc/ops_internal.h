@@ -1,0 +1,103 @@
+// Internal declarations of the operators of gecc_ops.h (gfx950 only).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include "gecc_ops.h"
+
+namespace gecc {
+
+// ---- microscaled 4-bit matrices (layout: gecc_ops.h) ------------------------------------------------
+constexpr int MX_PAD = 256;        // columns of a data row are padded to that many (128 bytes)
+constexpr int MX_UNIT = 512;       // columns of a scale tile
+__host__ __device__ inline int64_t mx_pad(int64_t cols) { return (cols + MX_PAD - 1) / MX_PAD * MX_PAD; }
+__host__ __device__ inline int64_t mx_units(int64_t cols) { return (mx_pad(cols) + MX_UNIT - 1) / MX_UNIT; }
+
+struct MxQuantArgs {
+  const void* X;
+  int dtype, rows, cols;
+  int64_t ld;
+  uint8_t *data, *scales, *t_data, *t_scales;
+};
+hipError_t launch_mx4_quantize(const MxQuantArgs& a, hipStream_t st);
+
+struct MxDequantArgs {
+  const uint8_t *data, *scales;
+  void* out;
+  int dtype, rows, cols;
+  int64_t ld;
+};
+hipError_t launch_mx4_dequantize(const MxDequantArgs& a, hipStream_t st);
+
+// Few rows: Y[n x m] = X W^T, n <= MX_FEW_ROWS.  X as a packed matrix or (x != null) raw, quantised on the way.
+constexpr int MX_FEW_ROWS = 64;
+struct MxFewArgs {
+  int n, k, m;
+  const void* x;                 // raw X, or null
+  int x_dtype;
+  int64_t ldx;
+  const uint8_t *x_data, *x_scales;
+  const uint8_t *w_data, *w_scales;
+  void* y;
+  int y_dtype;
+  int64_t ldy;
+};
+bool mx4_few_raw_ok(int n, int k);      // raw X small enough to be quantised by every workgroup
+hipError_t launch_mx4_few(const MxFewArgs& a, hipStream_t st);
+
+// ---- tiled products on 16-bit and 4-bit operands -----------------------------------------------------
+// D[i][j] = sum_k A(i, k) B(j, k), i < m_rows, j < n_rows, stored transposed: element (i, j) at out[j * ld + i].
+enum TileEpi {
+  EPI_OUT = 0,      // C: fp32 or bf16, the caller's leading dimension
+  EPI_GRAM = 1,     // S = acc * f_acc, fp16, both triangles (tiles below the diagonal are mirrored)
+  EPI_POLY = 2,     // b S + c S S: f_old * S(i, j) + f_acc * acc, fp16, both triangles
+  EPI_UPDATE = 3    // f_old * (hi + lo) + f_acc * acc -> hi, lo (two halves of 32 bits) or, in the last step, the output
+};
+struct TileArgs {
+  const uint8_t *A, *B;          // bytes; row r of a k-contiguous operand at r * ld
+  int64_t lda, ldb;              // bytes
+  int64_t sa, sb;                // bytes between batch items
+  const uint8_t *scale_a, *scale_b;   // 4-bit operands: scale tiles
+  int m_rows, n_rows;            // valid rows of A and of B
+  int a_cols, k_rows;            // A with its rows contiguous: rows it is stored with (a multiple of 64) and valid k, else unused
+  int stages;                    // k in stages of 128 bytes a row
+  int batch;
+  int split;                     // workgroups per tile, one range of stages each
+  float* part;                   // partial tiles of a split product
+  bool symmetric;                // only tiles with tile_m >= tile_n are computed
+  // epilogue
+  void* out;
+  int64_t ldo, so;               // elements
+  int out_dtype;                 // EPI_OUT, EPI_UPDATE's output
+  int m_store, n_store;          // elements stored (EPI_GRAM, EPI_POLY, EPI_UPDATE: the padding too)
+  float f_acc, f_old;
+  const uint16_t *old_hi, *old_lo;    // fp16; old_lo may be null
+  uint16_t* out_lo;              // or null
+  int64_t ld_old, s_old;         // elements
+  bool last, transpose_out;      // EPI_UPDATE: out is the caller's O (bf16 or fp32); element (i, j) at out[i * ldo + j]
+};
+enum TileKind { KIND_F16 = 0, KIND_MX4 = 1 };
+// tile edge (64 or 128) and split for a product, and the bytes of partial tiles it then needs
+struct TilePlan { int tile, split; size_t part_bytes; };
+TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, int stages, int batch, bool symmetric);
+hipError_t launch_tiles(TileKind kind, TileEpi epi, const TileArgs& a, const TilePlan& plan, hipStream_t st);
+
+// ---- the orthogonalised update -------------------------------------------------------------------------
+constexpr int ORTH_PARTS = 256;    // partial sums of squares of a batch item, at most
+struct OrthPrepArgs {
+  gecc_orth_params p;
+  const void* G;
+  float* M;                      // or null
+  double* parts;                 // [batch][nparts]
+  int nparts;
+  uint16_t *hi, *lo;             // X: [batch][s][lp], s = shorter side, lp = longer side padded to 64
+  int64_t lp;
+  int s, l;
+  bool tall;
+  float x_scale;                 // X is stored times this
+};
+hipError_t launch_orth_norm(const OrthPrepArgs& a, hipStream_t st);      // M, sums of squares of U
+hipError_t launch_orth_start(const OrthPrepArgs& a, hipStream_t st);     // X
+// O = scale * X where there are no steps
+hipError_t launch_orth_store(const OrthPrepArgs& a, void* out, hipStream_t st);
+
+}  // namespace gecc

@@ -1,0 +1,384 @@
+// Tiled products on fp16 and on microscaled 4-bit operands, D[i][j] = sum_k A(i, k) B(j, k), for the operators of
+// gecc_ops.h: tiles of 64 x 64 or 128 x 128, k shared out over several workgroups where there are few tiles.
+//
+// Both kinds of operand are 128 bytes of k a row and stage (64 fp16 or 256 four-bit values), and a fragment of either
+// kind is 16 bytes a lane (16 rows x 32 fp16 or x 128 four-bit values), so that one kernel serves both: the matrix
+// instructions take the same 16 cycles.  Operands travel HBM -> LDS directly, one stage ahead of the one in use.
+//
+// LDS of a stage, an operand: k-contiguous: [row][128 bytes], the eight 16-byte chunks of a row XOR-swizzled with
+// (row >> 1) & 7, so that the 16 rows of a fragment read meet in no bank.  A stored with its rows contiguous (fp16, tiles
+// of 128): [k][128 rows], read by the transposing LDS read, the 64-byte chunks XOR-swizzled with k & 3 and the 32-byte
+// halves of a chunk swapped when k & 8.  Scales of 4-bit operands: every second stage 16 bytes a row, the four bytes of
+// a lane (its block of four consecutive instructions) in one 32-bit read.
+//
+// A lane ends up with D[4 g .. 4 g + 3][l16] of every 16 x 16 block, so D is stored transposed: four consecutive values.
+#include <type_traits>
+#include "ops_internal.h"
+#include "dma_device.h"
+#include "ops_device.h"
+
+namespace gecc {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(8))) short s16x8_t;
+typedef __attribute__((ext_vector_type(8))) int i32x8_t;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+constexpr int THREADS = 256;
+
+// ---- what becomes of a tile: element (i, j) of D, four values i .. i + 3 a call -------------------------------------
+template <int EPI>
+__device__ __forceinline__ void store4(const TileArgs& a, int b, int i, int j, bool mirror, const f32x4_t& acc, bool vec_out) {
+  if (EPI == EPI_OUT) {
+    if (j >= a.n_rows || i >= a.m_rows) return;
+    if (a.out_dtype == GECC_F32) {
+      float* o = static_cast<float*>(a.out) + b * a.so + (int64_t)j * a.ldo + i;
+      if (vec_out && i + 4 <= a.m_rows) *reinterpret_cast<f32x4_t*>(o) = acc;
+      else
+        for (int v = 0; v < 4; ++v) if (i + v < a.m_rows) o[v] = acc[v];
+    } else {
+      uint16_t* o = static_cast<uint16_t*>(a.out) + b * a.so + (int64_t)j * a.ldo + i;
+      if (vec_out && i + 4 <= a.m_rows)
+        *reinterpret_cast<u32x2_t*>(o) = u32x2_t{(unsigned)to_bf16(acc[0]) | ((unsigned)to_bf16(acc[1]) << 16),
+                                                 (unsigned)to_bf16(acc[2]) | ((unsigned)to_bf16(acc[3]) << 16)};
+      else
+        for (int v = 0; v < 4; ++v) if (i + v < a.m_rows) o[v] = to_bf16(acc[v]);
+    }
+    return;
+  }
+  // (the internal matrices: i is stored in groups of four up to m_store, a multiple of 64)
+  if (j >= a.n_store || i >= a.m_store) return;
+  float x[4];
+  if (EPI == EPI_GRAM) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x[v] = a.f_acc * acc[v];
+  } else {
+    const int64_t at = b * a.s_old + (int64_t)j * a.ld_old + i;
+    const f16x4_t hi = *reinterpret_cast<const f16x4_t*>(a.old_hi + at);
+    f16x4_t lo = {0, 0, 0, 0};
+    if (EPI == EPI_UPDATE && a.old_lo) lo = *reinterpret_cast<const f16x4_t*>(a.old_lo + at);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x[v] = fmaf(a.f_old, (float)hi[v] + (float)lo[v], a.f_acc * acc[v]);
+  }
+  if (EPI == EPI_UPDATE && a.last) {
+    // (no loops over the four with a run-time end: the caller's rows and columns end anywhere)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      if (i + v >= a.m_rows || j >= a.n_rows) continue;
+      const int64_t at = b * a.so + (a.transpose_out ? (int64_t)(i + v) * a.ldo + j : (int64_t)j * a.ldo + i + v);
+      if (a.out_dtype == GECC_F32) static_cast<float*>(a.out)[at] = x[v];
+      else static_cast<uint16_t*>(a.out)[at] = to_bf16(x[v]);
+    }
+    return;
+  }
+  uint16_t* out = static_cast<uint16_t*>(a.out) + b * a.so;
+  f16x4_t h;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) h[v] = (_Float16)x[v];
+  *reinterpret_cast<f16x4_t*>(out + (int64_t)j * a.ldo + i) = h;
+  if (EPI == EPI_UPDATE) {
+    if (a.out_lo) {
+      f16x4_t l;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) l[v] = (_Float16)(x[v] - (float)h[v]);
+      *reinterpret_cast<f16x4_t*>(a.out_lo + b * a.so + (int64_t)j * a.ldo + i) = l;
+    }
+  } else if (mirror && j < a.m_store) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const _Float16 y = (_Float16)x[v];      // (not an element of h: this compiler's bit cast of one takes the first)
+      if (i + v < a.n_store) out[(int64_t)(i + v) * a.ldo + j] = __builtin_bit_cast(uint16_t, y);
+    }
+  }
+}
+
+// ---- operands --------------------------------------------------------------------------------------------------------
+// KC: k-contiguous.  Otherwise (T rows = 128, fp16): element (row, k) at P[k * ld + row].
+template <bool KC, int T>
+struct TileOperand {
+  static constexpr int NV = T * 128 / (THREADS * 16);     // DMA instructions of a wavefront per stage
+  const uint8_t* base;
+  int64_t step;                 // bytes from stage to stage
+  int64_t left;                 // bytes from `base` to the end of the operand
+  unsigned voff[NV];
+  int frag[T / 32];
+
+  __device__ __forceinline__ void init(const uint8_t* P, int64_t ld, int r0, int rows, int cols, int stage0, int sub) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+    if (KC) {
+      base = P + (int64_t)r0 * ld + (int64_t)stage0 * 128;
+      step = 128;
+      left = rows > r0 ? (int64_t)(rows - r0) * ld - (int64_t)stage0 * 128 : 0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int s = (wave * NV + i) * 64 + lane, row = s >> 3, c = (s & 7) ^ ((row >> 1) & 7);
+        voff[i] = r0 + row < rows ? (unsigned)(row * ld + c * 16) : OOB;
+      }
+#pragma unroll
+      for (int i = 0; i < T / 32; ++i) {
+        const int row = sub + i * 16 + l16;
+        frag[i] = row * 128 + ((g ^ ((row >> 1) & 7)) << 4);
+      }
+    } else {
+      base = P + (int64_t)stage0 * 64 * ld + (int64_t)r0 * 2;
+      step = 64 * ld;
+      left = (int64_t)(rows - stage0 * 64) * ld - (int64_t)r0 * 2;      // (rows: the valid k)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int s = (wave * NV + i) * 64 + lane, krow = s >> 4, p = s & 15;
+        const int u = (((p >> 2) ^ (krow & 3)) << 2) | ((p & 3) ^ (((krow >> 3) & 1) << 1));
+        voff[i] = r0 + u * 8 < cols ? (unsigned)(krow * ld + u * 16) : OOB;
+      }
+      const int j = (lane >> 2) & 3, q = lane & 3;
+#pragma unroll
+      for (int i = 0; i < T / 32; ++i) {
+        const int col = sub + i * 16 + 4 * q, krow = 8 * g + j, u = col >> 3;
+        frag[i] = krow * 256 + (((((u >> 2) ^ j) << 2) | ((u & 3) ^ ((g & 1) << 1))) << 4) + (col & 7) * 2;
+      }
+    }
+  }
+  // stage number t (from the range's first) into the LDS region at `lds`
+  __device__ __forceinline__ void issue(unsigned lds, int wave_u, int t) const {
+    const int64_t off = (int64_t)t * step, rest = left - off;
+    const i32x4_t rsrc = make_rsrc(base + off, rest <= 0 ? 0u : rest > 0x7fffffff ? 0x7fffffffu : (unsigned)rest);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) dma16(lds + (wave_u * NV + i) * 1024, voff[i], rsrc, 0);
+  }
+  // the 16 bytes a lane of fragment i (16 rows), instruction ks (0, 1) of the stage
+  __device__ __forceinline__ s16x8_t fragment(const char* region, int i, int ks) const {
+    if (KC) return *reinterpret_cast<const s16x8_t*>(region + (frag[i] ^ (ks << 6)));
+    const char* p = region + frag[i] + ks * 32 * 256;
+    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(p));
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(p + 4 * 256));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+};
+
+// the index of a tile in the lower triangle: tm >= tn
+__device__ __forceinline__ void triangle(int t, int& tm, int& tn) {
+  tm = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+  while (tm * (tm + 1) / 2 > t) --tm;
+  while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
+  tn = t - tm * (tm + 1) / 2;
+}
+
+template <int T>
+__device__ __forceinline__ void tile_at(const TileArgs& a, int t, int& tm, int& tn) {
+  if (a.symmetric) { triangle(t, tm, tn); return; }
+  const int ntm = (a.m_rows + T - 1) / T;
+  tm = t % ntm;
+  tn = t / ntm;
+}
+
+template <int KIND, bool KCA, int T, int EPI>
+__global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_out) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  constexpr int F = T / 32;                       // 16-row fragments of a wavefront, an operand
+  constexpr int STAGE = T * 128;                  // bytes of a stage, an operand
+  constexpr int SCALES = KIND == KIND_MX4 ? T * 16 : 0;
+  constexpr int SLOT = 2 * STAGE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+  const int wr = wave >> 1, wc = wave & 1, l16 = lane & 15, g = lane >> 4;
+  const int b = blockIdx.z;
+  int tm, tn;
+  tile_at<T>(a, blockIdx.x, tm, tn);
+  const int r0 = tm * T, c0 = tn * T;
+  // this workgroup's stages: a range of whole pairs (a scale tile is two stages long)
+  const int pairs = (a.stages + 1) / 2;
+  const int first = (int)((int64_t)pairs * blockIdx.y / a.split) * 2;
+  const int last = min((int)((int64_t)pairs * (blockIdx.y + 1) / a.split) * 2, a.stages);
+  const int count = last - first;
+
+  TileOperand<KCA, T> oa;
+  TileOperand<true, T> ob;
+  oa.init(a.A + b * a.sa, a.lda, r0, KCA ? a.m_rows : a.k_rows, a.a_cols, first, wr * (T / 2));
+  ob.init(a.B + b * a.sb, a.ldb, c0, a.n_rows, 0, first, wc * (T / 2));
+
+  // scales: instruction number `wave` of the 2 T / 64 of a pair (64 rows each); wavefronts beyond them repeat the last
+  const uint8_t* sbase = nullptr;
+  unsigned svoff = 0, slds = 0;
+  int64_t sleft = 0;
+  if (KIND == KIND_MX4) {
+    const int q = min(wave_u, 2 * T / 64 - 1), per = T / 64;
+    const bool is_b = q >= per;
+    const int row = (is_b ? q - per : q) * 64 + lane;
+    const int64_t units = pairs, row0 = is_b ? c0 : r0, rows16 = ((is_b ? a.n_rows : a.m_rows) + 15) / 16;
+    sbase = (is_b ? a.scale_b : a.scale_a) + (row0 / 16 * units + first / 2) * 256;
+    sleft = (rows16 - row0 / 16) * units * 256 - (int64_t)(first / 2) * 256;
+    svoff = (unsigned)((row >> 4) * units * 256 + (row & 15) * 16);
+    if (row0 / 16 + (row >> 4) >= rows16) svoff = OOB;
+    slds = (is_b ? SCALES : 0) + (unsigned)(is_b ? q - per : q) * 1024;
+  }
+
+  f32x4_t acc[F][F];
+#pragma unroll
+  for (int i = 0; i < F; ++i)
+#pragma unroll
+    for (int j = 0; j < F; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  auto issue = [&](int t) {
+    const unsigned at = lds0 + (t & 1) * SLOT;
+    if (KIND == KIND_MX4 && (t & 1) == 0) {
+      const int64_t off = (int64_t)(t >> 1) * 256, rest = sleft - off;
+      const i32x4_t rsrc = make_rsrc(sbase + off, rest <= 0 ? 0u : rest > 0x7fffffff ? 0x7fffffffu : (unsigned)rest);
+      dma16(lds0 + 2 * SLOT + ((t >> 1) & 1) * 2 * SCALES + slds, svoff, rsrc, 0);
+    }
+    oa.issue(at, wave_u, t);
+    ob.issue(at + STAGE, wave_u, t);
+  };
+  int sa[F], sb[F];
+#pragma unroll
+  for (int i = 0; i < F; ++i) sa[i] = sb[i] = 0;
+  auto multiply = [&](int t, auto odd_c) {
+    constexpr bool ODD = decltype(odd_c)::value;
+    const char* ra = smem + (ODD ? SLOT : 0);
+    const char* rb = ra + STAGE;
+    if (KIND == KIND_MX4 && !ODD) {
+      const char* rs = smem + 2 * SLOT + ((t >> 1) & 1) * 2 * SCALES;
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        sa[i] = *reinterpret_cast<const int*>(rs + (wr * (T / 2) + i * 16 + l16) * 16 + g * 4);
+        sb[i] = *reinterpret_cast<const int*>(rs + SCALES + (wc * (T / 2) + i * 16 + l16) * 16 + g * 4);
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      s16x8_t fa[F], fb[F];
+#pragma unroll
+      for (int i = 0; i < F; ++i) fa[i] = oa.fragment(ra, i, ks);
+#pragma unroll
+      for (int j = 0; j < F; ++j) fb[j] = ob.fragment(rb, j, ks);
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+          if (KIND == KIND_F16) {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, fa[i]), __builtin_bit_cast(f16x8_t, fb[j]), acc[i][j], 0, 0, 0);
+          } else {
+            const i32x4_t xa = __builtin_bit_cast(i32x4_t, fa[i]), xb = __builtin_bit_cast(i32x4_t, fb[j]);
+            const i32x8_t va = {xa[0], xa[1], xa[2], xa[3], 0, 0, 0, 0}, vb = {xb[0], xb[1], xb[2], xb[3], 0, 0, 0, 0};
+            // (the byte of the scale registers, 2 ODD + ks, is a constant of the instruction)
+            if (ks == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(va, vb, acc[i][j], 4, 4, ODD ? 2 : 0, sa[i], ODD ? 2 : 0, sb[j]);
+            else         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(va, vb, acc[i][j], 4, 4, ODD ? 3 : 1, sa[i], ODD ? 3 : 1, sb[j]);
+          }
+        }
+    }
+  };
+  auto step = [&](int t, auto odd_c) {
+    wait_vm<0>();                                        // stage t of this wavefront's loads
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // its reads of stage t - 1 are back
+    __builtin_amdgcn_s_barrier();                        // stage t complete for everyone, the other slot free
+    asm volatile("" ::: "memory");
+    if (t + 1 < count) issue(t + 1);
+    multiply(t, odd_c);
+  };
+  issue(0);
+  for (int t = 0; t < count; t += 2) {
+    step(t, std::false_type{});
+    if (t + 1 < count) step(t + 1, std::true_type{});
+  }
+
+  if (a.split > 1) {
+    // [batch][range][tile][fragment pair][lane] in the order of the registers; tile_finish_kernel adds the ranges up
+    const int64_t tiles = gridDim.x;
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + (((int64_t)b * a.split + blockIdx.y) * tiles + blockIdx.x) * (T * T / 4) + wave * (F * F * 64) + lane;
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int j = 0; j < F; ++j) p[(i * F + j) * 64] = acc[i][j];
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < F; ++i)
+#pragma unroll
+    for (int j = 0; j < F; ++j)
+      store4<EPI>(a, b, r0 + wr * (T / 2) + i * 16 + 4 * g, c0 + wc * (T / 2) + j * 16 + l16, tm != tn, acc[i][j], vec_out);
+}
+
+// Adds the ranges of a split product up, in their order, and stores the result: a wavefront per fragment pair.
+template <int T, int EPI>
+__global__ __launch_bounds__(256) void tile_finish_kernel(TileArgs a, bool vec_out, int tiles) {
+  constexpr int F = T / 32;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const int piece = blockIdx.x * 4 + (threadIdx.x >> 6);        // of tiles * 4 F F
+  const int b = blockIdx.y;
+  const int t = piece / (4 * F * F), r = piece % (4 * F * F);
+  if (t >= tiles) return;
+  int tm, tn;
+  tile_at<T>(a, t, tm, tn);
+  const int wave = r / (F * F), i = r % (F * F) / F, j = r % F;
+  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(a.part) + ((int64_t)b * a.split * tiles + t) * (T * T / 4) + r * 64 + lane;
+  f32x4_t s = p[0];
+  for (int q = 1; q < a.split; ++q) {
+    const f32x4_t x = p[(int64_t)q * tiles * (T * T / 4)];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) s[v] += x[v];
+  }
+  store4<EPI>(a, b, tm * T + (wave >> 1) * (T / 2) + i * 16 + 4 * g, tn * T + (wave & 1) * (T / 2) + j * 16 + l16, tm != tn, s, vec_out);
+}
+
+int64_t tiles_of(int64_t m_rows, int64_t n_rows, int T, bool symmetric) {
+  const int64_t tm = (m_rows + T - 1) / T, tn = (n_rows + T - 1) / T;
+  return symmetric ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+template <int KIND, bool KCA, int T, int EPI>
+hipError_t launch(const TileArgs& a, hipStream_t st) {
+  const int64_t tiles = tiles_of(a.m_rows, a.n_rows, T, a.symmetric);
+  if (tiles > 0x7fffffff || a.batch > 65535) return hipErrorInvalidValue;
+  bool vec = false;
+  if (EPI == EPI_OUT) {
+    const int es = a.out_dtype == GECC_F32 ? 4 : 2;
+    vec = reinterpret_cast<uintptr_t>(a.out) % (4 * es) == 0 && a.ldo % 4 == 0 && a.so % 4 == 0;
+  }
+  constexpr int lds = 2 * 2 * T * 128 + (KIND == KIND_MX4 ? 2 * 2 * T * 16 : 0);
+  auto kern = tile_kernel<KIND, KCA, T, EPI>;
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kern, dim3((unsigned)tiles, a.split, a.batch), dim3(THREADS), lds, st, a, vec);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.split == 1) return e;
+  constexpr int F = T / 32;
+  hipLaunchKernelGGL((tile_finish_kernel<T, EPI>), dim3((unsigned)(tiles * F * F), a.batch), dim3(256), 0, st, a, vec, (int)tiles);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, int stages, int batch, bool symmetric) {
+  TilePlan p;
+  // 128 x 128 tiles once they fill the chip; A with its rows contiguous has no others
+  p.tile = epi == EPI_UPDATE || tiles_of(m_rows, n_rows, 128, symmetric) * batch >= 256 ? 128 : 64;
+  const int64_t tiles = tiles_of(m_rows, n_rows, p.tile, symmetric) * batch;
+  const int pairs = (stages + 1) / 2;
+  int64_t s = 512 / tiles;
+  if (s > 16) s = 16;
+  if (s > pairs / 2) s = pairs / 2;
+  p.split = s < 1 ? 1 : (int)s;
+  p.part_bytes = p.split > 1 ? (size_t)tiles * p.split * p.tile * p.tile * 4 : 0;
+  (void)kind;
+  return p;
+}
+
+hipError_t launch_tiles(TileKind kind, TileEpi epi, const TileArgs& a0, const TilePlan& plan, hipStream_t st) {
+  TileArgs a = a0;
+  a.split = plan.split;
+  if (kind == KIND_MX4) {
+    return plan.tile == 128 ? launch<KIND_MX4, true, 128, EPI_OUT>(a, st) : launch<KIND_MX4, true, 64, EPI_OUT>(a, st);
+  }
+  switch (epi) {
+    case EPI_GRAM: return plan.tile == 128 ? launch<KIND_F16, true, 128, EPI_GRAM>(a, st) : launch<KIND_F16, true, 64, EPI_GRAM>(a, st);
+    case EPI_POLY: return plan.tile == 128 ? launch<KIND_F16, true, 128, EPI_POLY>(a, st) : launch<KIND_F16, true, 64, EPI_POLY>(a, st);
+    case EPI_UPDATE: return launch<KIND_F16, false, 128, EPI_UPDATE>(a, st);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace gecc

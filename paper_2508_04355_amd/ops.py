@@ -1,0 +1,259 @@
+"""Operators around a layer's products (include/gecc_ops.h): microscaled 4-bit quantisation, products on such operands in
+training and serving, and the orthogonalised update of the layer's weight.
+
+Argument checks and marshalling only; everything is computed by the HIP kernels of libgecc on torch's current stream.
+Outputs and workspaces come from torch's allocator, which keeps their memory in stream order; nothing is kept between calls.
+There is no CPU fallback.
+"""
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from . import gecc
+from .gecc import BF16, F32, GeccError, _check, _ptr, _stream
+
+ORTH_MAX_STEPS = 16
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+class OrthParams(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("batch", C.c_int32), ("dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("steps", C.c_int32), ("nesterov", C.c_int32), ("reserved", C.c_int32),
+                ("ld_g", C.c_int64), ("ld_m", C.c_int64), ("ld_o", C.c_int64),
+                ("stride_g", C.c_int64), ("stride_m", C.c_int64), ("stride_o", C.c_int64),
+                ("mu", C.c_float), ("eps", C.c_float), ("scale", C.c_float), ("a", C.c_float), ("b", C.c_float), ("c", C.c_float)]
+
+
+_SYMBOLS = ["gecc_mx4_data_bytes", "gecc_mx4_scale_bytes", "gecc_mx4_quantize", "gecc_mx4_dequantize", "gecc_mx4_gemm_workspace",
+            "gecc_mx4_gemm", "gecc_mx4_linear_workspace", "gecc_mx4_linear", "gecc_mx4_linear_backward_workspace",
+            "gecc_mx4_linear_backward", "gecc_orthogonalize_workspace", "gecc_orthogonalize"]
+_lib = None
+
+
+def lib():
+    """libgecc with the signatures of gecc_ops.h; raises if the library is not built."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    L = gecc.lib()
+    vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+    for f in ("gecc_mx4_data_bytes", "gecc_mx4_scale_bytes"):
+        getattr(L, f).argtypes = [i32, i32]
+    for f in ("gecc_mx4_gemm_workspace", "gecc_mx4_linear_workspace", "gecc_mx4_linear_backward_workspace"):
+        getattr(L, f).argtypes = [i32, i32, i32]
+    L.gecc_orthogonalize_workspace.argtypes = [C.POINTER(OrthParams)]
+    L.gecc_mx4_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp]
+    L.gecc_mx4_dequantize.argtypes = [vp, vp, i32, i32, vp, i32, i64, vp]
+    L.gecc_mx4_gemm.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, i32, i64, vp, sz, vp]
+    L.gecc_mx4_linear.argtypes = [i32, i32, i32, vp, i32, i64, vp, vp, vp, i32, i64, vp, sz, vp]
+    L.gecc_mx4_linear_backward.argtypes = [i32, i32, i32, vp, i32, i64, vp, vp, vp, vp, vp, i32, i64, vp, i64, vp, sz, vp]
+    L.gecc_orthogonalize.argtypes = [C.POINTER(OrthParams), vp, vp, vp, vp, sz, vp]
+    for f in _SYMBOLS:
+        getattr(L, f).restype = sz if f.endswith(("_bytes", "_workspace")) else C.c_int
+    _lib = L
+    return L
+
+
+def _matrix(t, what, dtypes=_DTYPES):
+    """`t` as a device matrix whose rows are contiguous (a copy only where its last dimension is strided)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise GeccError("%s: a tensor on the GPU is wanted" % what)
+    if t.dim() != 2:
+        raise GeccError("%s: a matrix is wanted, got %d dimensions" % (what, t.dim()))
+    if t.dtype not in dtypes:
+        raise GeccError("%s: %s is not supported (float32 and bfloat16 are)" % (what, t.dtype))
+    return _rows(t)
+
+
+def _rows(t):
+    # (torch leaves the strides of dimensions of length 1 open)
+    ok = (t.shape[-1] <= 1 or t.stride(-1) == 1) and (t.shape[-2] <= 1 or t.stride(-2) >= t.shape[-1])
+    return t if ok else t.contiguous()
+
+
+def _ld(t):
+    return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+
+
+def _output(out, shape, dtype, device, what):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if out.device != device or tuple(out.shape) != tuple(shape) or out.dtype not in _DTYPES or out.data_ptr() != _rows(out).data_ptr():
+        raise GeccError("%s: out has to be a float32 or bfloat16 tensor of shape %s with contiguous rows on %s" % (what, tuple(shape), device))
+    return out
+
+
+def _workspace(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _aligned(ws):
+    # (torch's allocator hands out multiples of 512 bytes)
+    return _ptr(ws), 0 if ws is None else ws.numel()
+
+
+class Mx4:
+    """A matrix of `rows` rows in microscaled 4-bit floating point, blocks of 32 along its columns: two uint8 buffers in
+    the layout of include/gecc_ops.h."""
+
+    def __init__(self, data: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
+        self.data, self.scales, self.rows, self.cols = data, scales, int(rows), int(cols)
+        for t, f, what in ((data, "gecc_mx4_data_bytes", "data"), (scales, "gecc_mx4_scale_bytes", "scales")):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous():
+                raise GeccError("Mx4: %s has to be a contiguous uint8 tensor on the GPU" % what)
+            need = getattr(lib(), f)(self.rows, self.cols)
+            if need == 0 or t.numel() != need:
+                raise GeccError("Mx4: %s of a %d x %d matrix has %d bytes, got %d" % (what, rows, cols, need, t.numel()))
+        if data.device != scales.device:
+            raise GeccError("Mx4: data and scales are on different devices")
+
+    @property
+    def shape(self):
+        return self.rows, self.cols
+
+    @property
+    def device(self):
+        return self.data.device
+
+
+def _new_mx4(rows, cols, device):
+    L = lib()
+    q = Mx4.__new__(Mx4)
+    q.rows, q.cols = rows, cols
+    q.data = torch.empty(L.gecc_mx4_data_bytes(rows, cols), dtype=torch.uint8, device=device)
+    q.scales = torch.empty(L.gecc_mx4_scale_bytes(rows, cols), dtype=torch.uint8, device=device)
+    return q
+
+
+def _mx4(q, what):
+    if not isinstance(q, Mx4):
+        raise GeccError("%s: an Mx4 matrix is wanted" % what)
+    return q
+
+
+def _one_device(what, *ts):
+    d = ts[0].device
+    if any(t is not None and t.device != d for t in ts):
+        raise GeccError("%s: operands on different devices" % what)
+    if d.index != torch.cuda.current_device():
+        raise GeccError("%s: operands are on %s, the current device is cuda:%d" % (what, d, torch.cuda.current_device()))
+    return d
+
+
+def mx4_quantize(x: torch.Tensor, both: bool = False):
+    """x (float32 or bfloat16, rows x cols) as an Mx4 matrix, blocks along its rows; with `both` also its transpose (blocks
+    along the columns of x), from one pass over x: (Q, Qt)."""
+    x = _matrix(x, "mx4_quantize")
+    d = _one_device("mx4_quantize", x)
+    rows, cols = x.shape
+    q = _new_mx4(rows, cols, d)
+    t = _new_mx4(cols, rows, d) if both else None
+    _check(lib().gecc_mx4_quantize(_ptr(x), _DTYPES[x.dtype], rows, cols, _ld(x), _ptr(q.data), _ptr(q.scales),
+                                   _ptr(t.data) if both else 0, _ptr(t.scales) if both else 0, _stream()))
+    return (q, t) if both else q
+
+
+def mx4_dequantize(q: Mx4, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values of an Mx4 matrix (exact in both types)."""
+    _mx4(q, "mx4_dequantize")
+    d = _one_device("mx4_dequantize", q)
+    out = _output(out, q.shape, dtype, d, "mx4_dequantize")
+    if out.dtype not in _DTYPES:
+        raise GeccError("mx4_dequantize: %s is not supported" % out.dtype)
+    _check(lib().gecc_mx4_dequantize(_ptr(q.data), _ptr(q.scales), q.rows, q.cols, _ptr(out), _DTYPES[out.dtype], _ld(out), _stream()))
+    return out
+
+
+def mx4_gemm(a: Mx4, b: Mx4, dtype=torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A B^T: (n x k) and (m x k) to n x m, sums in fp32."""
+    _mx4(a, "mx4_gemm"), _mx4(b, "mx4_gemm")
+    if a.cols != b.cols:
+        raise GeccError("mx4_gemm: %d columns against %d" % (a.cols, b.cols))
+    d = _one_device("mx4_gemm", a, b)
+    n, k, m = a.rows, a.cols, b.rows
+    out = _output(out, (n, m), dtype, d, "mx4_gemm")
+    if out.dtype not in _DTYPES:
+        raise GeccError("mx4_gemm: %s is not supported" % out.dtype)
+    ws = _workspace(lib().gecc_mx4_gemm_workspace(n, k, m), d)
+    _check(lib().gecc_mx4_gemm(n, k, m, _ptr(a.data), _ptr(a.scales), _ptr(b.data), _ptr(b.scales), _ptr(out), _DTYPES[out.dtype], _ld(out),
+                               *_aligned(ws), _stream()))
+    return out
+
+
+def mx4_linear(x: torch.Tensor, w: Mx4, dtype=None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Q(x) w^T: tokens (n x k, float32 or bfloat16, quantised on the way) through a layer whose weight (m x k) is kept in 4
+    bits; n x m of `dtype` (x's own by default).  No tokens: an empty result."""
+    x, _ = _matrix(x, "mx4_linear"), _mx4(w, "mx4_linear")
+    if x.shape[1] != w.cols:
+        raise GeccError("mx4_linear: tokens of %d values against a weight of %d columns" % (x.shape[1], w.cols))
+    d = _one_device("mx4_linear", x, w)
+    n, k, m = x.shape[0], w.cols, w.rows
+    out = _output(out, (n, m), x.dtype if dtype is None else dtype, d, "mx4_linear")
+    if out.dtype not in _DTYPES:
+        raise GeccError("mx4_linear: %s is not supported" % out.dtype)
+    if n == 0:
+        return out
+    ws = _workspace(lib().gecc_mx4_linear_workspace(n, k, m), d)
+    _check(lib().gecc_mx4_linear(n, k, m, _ptr(x), _DTYPES[x.dtype], _ld(x), _ptr(w.data), _ptr(w.scales), _ptr(out), _DTYPES[out.dtype],
+                                 _ld(out), *_aligned(ws), _stream()))
+    return out
+
+
+def mx4_linear_backward(dy: torch.Tensor, wt: Optional[Mx4], xt: Optional[Mx4], dtype=None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """The layer's gradients, straight through the roundings: dx = Q(dy) W (n x k, of `dtype`, dy's own by default) and
+    dw = Q(dy^T) X (m x k, fp32).  wt, xt: the second matrices of mx4_quantize(w, both=True) and mx4_quantize(x,
+    both=True).  Either may be None; its gradient is then None too."""
+    dy = _matrix(dy, "mx4_linear_backward")
+    n, m = dy.shape
+    if wt is None and xt is None:
+        raise GeccError("mx4_linear_backward: neither gradient is wanted")
+    for q, size, what in ((wt, m, "wt"), (xt, n, "xt")):
+        if q is not None and (not isinstance(q, Mx4) or q.cols != size):
+            raise GeccError("mx4_linear_backward: %s has to be an Mx4 matrix of %d columns" % (what, size))
+    if wt is not None and xt is not None and wt.rows != xt.rows:
+        raise GeccError("mx4_linear_backward: wt has %d rows, xt %d" % (wt.rows, xt.rows))
+    d = _one_device("mx4_linear_backward", dy, wt, xt)
+    k = (wt if wt is not None else xt).rows
+    dtype = dy.dtype if dtype is None else dtype
+    if dtype not in _DTYPES:
+        raise GeccError("mx4_linear_backward: %s is not supported" % dtype)
+    dx = torch.empty((n, k), dtype=dtype, device=d) if wt is not None else None
+    dw = torch.empty((m, k), dtype=torch.float32, device=d) if xt is not None else None
+    ws = _workspace(lib().gecc_mx4_linear_backward_workspace(n, k, m), d)
+    _check(lib().gecc_mx4_linear_backward(n, k, m, _ptr(dy), _DTYPES[dy.dtype], _ld(dy), _ptr(wt and wt.data), _ptr(wt and wt.scales),
+                                          _ptr(xt and xt.data), _ptr(xt and xt.scales), _ptr(dx), _DTYPES[dtype], k, _ptr(dw), k,
+                                          *_aligned(ws), _stream()))
+    return dx, dw
+
+
+def orthogonalize(g: torch.Tensor, momentum: Optional[torch.Tensor] = None, mu: float = 0.95, nesterov: bool = True, steps: int = 5,
+                  coefficients: Tuple[float, float, float] = (3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale: float = 1.0,
+                  dtype=torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The orthogonalised update of a weight (rows x cols, or a batch of them) from its gradient g (float32 or bfloat16):
+    momentum (fp32 of g's shape, updated in place; or None), Frobenius normalisation and `steps` of
+    X <- a X + (b S + c S S) X, S = X X^T, on the shorter side; `scale` times the result."""
+    if not isinstance(g, torch.Tensor) or not g.is_cuda or g.dim() not in (2, 3) or g.dtype not in _DTYPES:
+        raise GeccError("orthogonalize: g has to be a float32 or bfloat16 matrix, or a batch of them, on the GPU")
+    if 0 in g.shape:
+        raise GeccError("orthogonalize: an empty matrix")
+    g = _rows(g)
+    d = _one_device("orthogonalize", g, momentum)
+    if momentum is not None and (momentum.dtype != torch.float32 or momentum.shape != g.shape or _rows(momentum) is not momentum):
+        raise GeccError("orthogonalize: the momentum has to be a float32 tensor of g's shape with contiguous rows")
+    out = _output(out, g.shape, dtype, d, "orthogonalize")
+    if out.dtype not in _DTYPES:
+        raise GeccError("orthogonalize: %s is not supported" % out.dtype)
+    rows, cols = g.shape[-2:]
+    batch = g.shape[0] if g.dim() == 3 else 1
+
+    def stride(t):
+        return t.stride(0) if t is not None and t.dim() == 3 and batch > 1 else 0
+    p = OrthParams(rows=rows, cols=cols, batch=batch, dtype=_DTYPES[g.dtype], out_dtype=_DTYPES[out.dtype], steps=steps,
+                   nesterov=1 if nesterov else 0, reserved=0, ld_g=_ld(g), ld_m=_ld(momentum) if momentum is not None else 0, ld_o=_ld(out),
+                   stride_g=stride(g), stride_m=stride(momentum), stride_o=stride(out), mu=mu, eps=eps, scale=scale,
+                   a=coefficients[0], b=coefficients[1], c=coefficients[2])
+    nbytes = lib().gecc_orthogonalize_workspace(C.byref(p))
+    ws = _workspace(nbytes, d)
+    _check(lib().gecc_orthogonalize(C.byref(p), _ptr(g), _ptr(momentum), _ptr(out), *_aligned(ws), _stream()))
+    return out
