@@ -86,7 +86,7 @@ struct OrthPlan {
   int nparts;
   TilePlan gram, poly, update;
   size_t parts, x[2], lo[2], gram_at, poly_at, part, total;
-  float sx[GECC_ORTH_MAX_STEPS + 1], ss[GECC_ORTH_MAX_STEPS], sp_[GECC_ORTH_MAX_STEPS];    // powers of two that X, S, P are stored with
+  OrthSteps steps;
 };
 
 // a power of two that brings values up to `most` to at most half of fp16's range
@@ -97,19 +97,29 @@ float power_for(double most) {
 
 // X has no singular value above 1 (its Frobenius norm is at most 1), and a step maps each by a polynomial: the largest
 // value of the polynomials over what is reached bounds every element of X, S and P, whatever the data.
-bool orth_scales(const gecc_orth_params& p, OrthPlan* o) {
+//
+// P takes a part f of the term a X along, P = b S + c S S + f a I, and the update the rest, X <- (1 - f) a X + P X, with the
+// X of the first term in 32 bits and the others in fp16.  f = 0: small singular values, which a early step hardly changes
+// but all later ones amplify, keep their 22 bits.  f = 1: where the singular values have arrived, a X and (b S + c S S) X
+// all but cancel, and the rounding of their small sum is smaller than that of the parts.  So f = 0 up to the last two
+// steps, 1/2, 1.  (128 x 128 noise: error 1.64e-3 with f = 0 throughout, 1.25e-3; a matrix of rank 64, 512 x 1536: 1.0e-3
+// and 1.7e-3, 1.1e-2 with f = 1 in the last three.)  For the same reason P is made from the S that was rounded, not from
+// its fp32 sums: an error in S that is in both terms moves the singular values along the polynomial, whose slope is small
+// there (from the sums: 1.70e-3).
+bool orth_steps(const gecc_orth_params& p, OrthSteps* o) {
   double sig = 1.0;
   for (int t = 0; t < p.steps; ++t) {
     sig *= 1.0 + 0x1p-6;          // rounding, and maxima between the points
+    o->fold[t] = t + 1 == p.steps ? 1.f : t + 2 == p.steps ? 0.5f : 0.f;
     o->sx[t] = power_for(sig);
     o->ss[t] = power_for(sig * sig);
     double next = 0.0, poly = 0.0;
     for (int i = 0; i <= 2048; ++i) {
       const double x = sig * i / 2048, y = x * x, q = (double)p.b * y + (double)p.c * y * y;
-      poly = std::fmax(poly, std::fabs(q));
+      poly = std::fmax(poly, std::fabs(q + o->fold[t] * (double)p.a));
       next = std::fmax(next, std::fabs(x * ((double)p.a + q)));
     }
-    o->sp_[t] = power_for(poly * (1.0 + 0x1p-6));
+    o->sp[t] = power_for(poly * (1.0 + 0x1p-6));
     if (!(next <= 16.0) || !(poly <= 4096.0)) return false;
     sig = next;
   }
@@ -123,16 +133,18 @@ bool orth_plan(const gecc_orth_params* p, OrthPlan* o) {
   if (p->steps < 0 || p->steps > GECC_ORTH_MAX_STEPS || (p->nesterov != 0 && p->nesterov != 1)) return false;
   if (!std::isfinite(p->mu) || !std::isfinite(p->scale) || !(p->eps > 0) || !std::isfinite(p->eps)) return false;
   if (!std::isfinite(p->a) || !std::isfinite(p->b) || !std::isfinite(p->c)) return false;
-  if (!orth_scales(*p, o)) return false;
+  if (!orth_steps(*p, &o->steps)) return false;
   o->tall = p->rows > p->cols;
   o->s = o->tall ? p->cols : p->rows;
   o->l = o->tall ? p->rows : p->cols;
   o->sp = align_up(o->s, 64);
   o->lp = align_up(o->l, 64);
   const int64_t elements = (int64_t)p->rows * p->cols;
-  int64_t parts = (elements + 8191) / 8192;
-  // (256 workgroups in all are few, a partial sum for each of them at every start of the next pass is not)
-  o->nparts = (int)(parts > ORTH_PARTS ? ORTH_PARTS : parts);
+  // a workgroup per 2048 elements (eight a thread), up to four a compute unit in all
+  const int64_t parts = (elements + 2047) / 2048, most = p->batch >= ORTH_PARTS ? 1 : ORTH_PARTS / p->batch;
+  o->nparts = (int)(parts > most ? most : parts);
+  o->total = 0;
+  if (orth_small_ok(o->s, o->l)) return true;
   o->gram = plan_tiles(KIND_F16, EPI_GRAM, o->s, o->s, (int)(o->lp / 64), p->batch, true);
   o->poly = plan_tiles(KIND_F16, EPI_POLY, o->s, o->s, (int)(o->sp / 64), p->batch, true);
   o->update = plan_tiles(KIND_F16, EPI_UPDATE, o->l, o->s, (int)(o->sp / 64), p->batch, false);
@@ -265,13 +277,13 @@ int gecc_mx4_linear_backward(int32_t n, int32_t k, int32_t m, const void* dev_dY
 }
 
 size_t gecc_orthogonalize_workspace(const gecc_orth_params* p) {
-  OrthPlan o;
+  OrthPlan o{};
   return orth_plan(p, &o) ? o.total : 0;
 }
 
 int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_M, void* dev_O, void* dev_workspace,
                        size_t workspace_bytes, void* stream) {
-  OrthPlan o;
+  OrthPlan o{};
   if (!orth_plan(p, &o) || !dev_G || !dev_O) return GECC_ERR_ARG;
   if (p->ld_g < p->cols || p->ld_o < p->cols || (dev_M && p->ld_m < p->cols)) return GECC_ERR_ARG;
   if (p->batch > 1 && (p->stride_g < p->rows * p->ld_g || p->stride_o < p->rows * p->ld_o || (dev_M && p->stride_m < p->rows * p->ld_m)))
@@ -290,7 +302,8 @@ int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_
   prep.parts = reinterpret_cast<double*>(ws + o.parts);
   prep.nparts = o.nparts;
   prep.s = o.s; prep.l = o.l; prep.lp = o.lp; prep.tall = o.tall;
-  prep.x_scale = o.sx[0];
+  prep.x_scale = o.steps.sx[0];
+  if (orth_small_ok(o.s, o.l)) return hip_rc(launch_orth_small(prep, dev_O, o.steps, st));
   hipError_t e = launch_orth_norm(prep, st);
   if (e != hipSuccess) return hip_rc(e);
   if (p->steps == 0) return hip_rc(launch_orth_store(prep, dev_O, st));
@@ -302,7 +315,7 @@ int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_
   for (int t = 0; t < p->steps && e == hipSuccess; ++t) {
     const int cur = t & 1;
     const bool last = t + 1 == p->steps;
-    const float sx = o.sx[t], ss = o.ss[t], sp = o.sp_[t];
+    const float sx = o.steps.sx[t], ss = o.steps.ss[t], sp = o.steps.sp[t], fold = o.steps.fold[t];
     TileArgs g{};
     g.A = g.B = reinterpret_cast<const uint8_t*>(half(o.x[cur]));
     g.lda = g.ldb = o.lp * 2;
@@ -328,6 +341,7 @@ int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_
     q.ld_old = o.sp; q.s_old = qs;
     q.f_old = (float)((double)p->b * sp / ss);
     q.f_acc = (float)((double)p->c * sp / ((double)ss * ss));
+    q.f_eye = fold * p->a * sp;
     e = launch_tiles(KIND_F16, EPI_POLY, q, o.poly, st);
     if (e != hipSuccess) break;
     TileArgs u{};
@@ -340,14 +354,15 @@ int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_
     u.stages = (int)(o.sp / 64);
     u.batch = p->batch;
     u.part = g.part;
-    u.old_hi = half(o.x[cur]);
-    // (the last step's X is in one half: nothing grows what its rounding adds any more)
-    u.old_lo = t == 0 || !last ? half(o.lo[cur]) : nullptr;
+    if (fold < 1.f) {           // (in the last step all of a X is in P: it needs no second half of X)
+      u.old_hi = half(o.x[cur]);
+      u.old_lo = half(o.lo[cur]);
+    }
     u.ld_old = o.lp; u.s_old = xs;
     u.m_store = (int)o.lp; u.n_store = o.s;
     u.last = last;
-    const double to = last ? (double)p->scale : (double)o.sx[t + 1];
-    u.f_old = (float)(to * p->a / sx);
+    const double to = last ? (double)p->scale : (double)o.steps.sx[t + 1];
+    u.f_old = (float)(to * (1.0 - fold) * p->a / sx);
     u.f_acc = (float)(to / ((double)sp * sx));
     if (last) {
       u.out = dev_O;

@@ -49,7 +49,7 @@ hipError_t launch_mx4_few(const MxFewArgs& a, hipStream_t st);
 enum TileEpi {
   EPI_OUT = 0,      // C: fp32 or bf16, the caller's leading dimension
   EPI_GRAM = 1,     // S = acc * f_acc, fp16, both triangles (tiles below the diagonal are mirrored)
-  EPI_POLY = 2,     // b S + c S S: f_old * S(i, j) + f_acc * acc, fp16, both triangles
+  EPI_POLY = 2,     // b S + c S S + f a I: f_old * S(i, j) + f_acc * acc + f_eye (i == j), fp16, both triangles
   EPI_UPDATE = 3    // f_old * (hi + lo) + f_acc * acc -> hi, lo (two halves of 32 bits) or, in the last step, the output
 };
 struct TileArgs {
@@ -69,8 +69,8 @@ struct TileArgs {
   int64_t ldo, so;               // elements
   int out_dtype;                 // EPI_OUT, EPI_UPDATE's output
   int m_store, n_store;          // elements stored (EPI_GRAM, EPI_POLY, EPI_UPDATE: the padding too)
-  float f_acc, f_old;
-  const uint16_t *old_hi, *old_lo;    // fp16; old_lo may be null
+  float f_acc, f_old, f_eye;     // f_eye: added to the diagonal (EPI_POLY)
+  const uint16_t *old_hi, *old_lo;    // fp16; EPI_UPDATE: both null where f_old is 0
   uint16_t* out_lo;              // or null
   int64_t ld_old, s_old;         // elements
   bool last, transpose_out;      // EPI_UPDATE: out is the caller's O (bf16 or fp32); element (i, j) at out[i * ldo + j]
@@ -82,7 +82,11 @@ TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, 
 hipError_t launch_tiles(TileKind kind, TileEpi epi, const TileArgs& a, const TilePlan& plan, hipStream_t st);
 
 // ---- the orthogonalised update -------------------------------------------------------------------------
-constexpr int ORTH_PARTS = 256;    // partial sums of squares of a batch item, at most
+constexpr int ORTH_PARTS = 1024;   // partial sums of squares, over all batch items where there are fewer than that
+// by step: the powers of two that X, S and P are stored times, and the part of a X that P takes along
+struct OrthSteps {
+  float sx[GECC_ORTH_MAX_STEPS + 1], ss[GECC_ORTH_MAX_STEPS], sp[GECC_ORTH_MAX_STEPS], fold[GECC_ORTH_MAX_STEPS];
+};
 struct OrthPrepArgs {
   gecc_orth_params p;
   const void* G;
@@ -97,6 +101,9 @@ struct OrthPrepArgs {
 };
 hipError_t launch_orth_norm(const OrthPrepArgs& a, hipStream_t st);      // M, sums of squares of U
 hipError_t launch_orth_start(const OrthPrepArgs& a, hipStream_t st);     // X
+// all of it in one launch, for matrices of up to 128 x 256
+bool orth_small_ok(int s, int l);
+hipError_t launch_orth_small(const OrthPrepArgs& a, void* out, const OrthSteps& steps, hipStream_t st);
 // O = scale * X where there are no steps
 hipError_t launch_orth_store(const OrthPrepArgs& a, void* out, hipStream_t st);
 

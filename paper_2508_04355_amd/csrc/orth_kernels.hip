@@ -3,13 +3,14 @@
 // (the second time out of the memory-side cache where they fit it), M and the two halves of X written once.
 #include "ops_internal.h"
 #include "ops_device.h"
+#include "lds_limit.h"
 
 namespace gecc {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 
-constexpr int CHUNK = 2048;     // columns of a workgroup's piece of a row: eight a thread
+constexpr int NORM_PIECES = 4;
 
 template <bool BF16G, bool VEC>
 __device__ __forceinline__ void load_g(const OrthPrepArgs& a, int b, int64_t row, int c, bool ok, float (&g)[8]) {
@@ -24,32 +25,46 @@ template <bool BF16G, bool VEC>
 __global__ __launch_bounds__(256) void orth_norm_kernel(OrthPrepArgs a) {
   __shared__ double red[4];
   const int b = blockIdx.y, tid = threadIdx.x;
-  const int64_t per_row = (a.p.cols + CHUNK - 1) / CHUNK, pieces = a.p.rows * per_row;
+  // pieces of eight columns; NORM_PIECES of them a thread and round, their loads on the way together
+  const unsigned per_row = (a.p.cols + 7) / 8;
+  const int64_t pieces = (int64_t)a.p.rows * per_row, step = (int64_t)gridDim.x * 256;
   float* M = a.M ? a.M + (int64_t)b * a.p.stride_m : nullptr;
   double sum = 0.0;
-  for (int64_t q = blockIdx.x; q < pieces; q += gridDim.x) {
-    const int64_t row = q / per_row;
-    const int c = (int)(q - row * per_row) * CHUNK + tid * 8;
-    if (c >= a.p.cols) continue;
-    float g[8], m[8];
-    load_g<BF16G, VEC>(a, b, row, c, true, g);
-    if (M) {
-      load8<true, VEC>(M, row * a.p.ld_m + c, c, a.p.cols, true, m);
+  for (int64_t q0 = (int64_t)blockIdx.x * 256 + tid; q0 < pieces; q0 += NORM_PIECES * step) {
+    float g[NORM_PIECES][8], m[NORM_PIECES][8];
+    int64_t row[NORM_PIECES];
+    int c[NORM_PIECES];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m[i] = fmaf(a.p.mu, m[i], g[i]);
-      float* o = M + row * a.p.ld_m + c;
-      if (VEC && c + 8 <= a.p.cols) {
-        reinterpret_cast<f32x4_t*>(o)[0] = f32x4_t{m[0], m[1], m[2], m[3]};
-        reinterpret_cast<f32x4_t*>(o)[1] = f32x4_t{m[4], m[5], m[6], m[7]};
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (c + i < a.p.cols) o[i] = m[i];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = update_of(a, g[i], m[i]);
+    for (int h = 0; h < NORM_PIECES; ++h) {
+      const int64_t q = q0 + h * step;
+      const bool ok = q < pieces;
+      // (pieces < 2^32 of most matrices: a division in 32 bits)
+      row[h] = q >> 32 ? q / per_row : (int64_t)((unsigned)q / per_row);
+      c[h] = (int)(q - row[h] * per_row) * 8;
+      load_g<BF16G, VEC>(a, b, row[h], c[h], ok, g[h]);
+      if (M) load8<true, VEC>(M, row[h] * a.p.ld_m + c[h], c[h], a.p.cols, ok, m[h]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) if (c + i < a.p.cols) sum = fma((double)g[i], (double)g[i], sum);
+    for (int h = 0; h < NORM_PIECES; ++h) {
+      if (q0 + h * step >= pieces) break;
+      if (M) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[h][i] = fmaf(a.p.mu, m[h][i], g[h][i]);
+        float* o = M + row[h] * a.p.ld_m + c[h];
+        if (VEC && c[h] + 8 <= a.p.cols) {
+          reinterpret_cast<f32x4_t*>(o)[0] = f32x4_t{m[h][0], m[h][1], m[h][2], m[h][3]};
+          reinterpret_cast<f32x4_t*>(o)[1] = f32x4_t{m[h][4], m[h][5], m[h][6], m[h][7]};
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) if (c[h] + i < a.p.cols) o[i] = m[h][i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[h][i] = update_of(a, g[h][i], m[h][i]);
+      }
+      // (values beyond the row are zeros: so is what the update makes of them)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fma((double)g[h][i], (double)g[h][i], sum);
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
@@ -61,7 +76,8 @@ __global__ __launch_bounds__(256) void orth_norm_kernel(OrthPrepArgs a) {
 // times / (|U| + eps), the same for every workgroup of a batch item
 __device__ __forceinline__ float normaliser(const OrthPrepArgs& a, int b, float times, double* red) {
   const int tid = threadIdx.x;
-  double s = tid < a.nparts ? a.parts[(int64_t)b * a.nparts + tid] : 0.0;
+  double s = 0.0;
+  for (int q = tid; q < a.nparts; q += 256) s += a.parts[(int64_t)b * a.nparts + q];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if ((tid & 63) == 0) red[tid >> 6] = s;
@@ -142,6 +158,230 @@ __global__ __launch_bounds__(256) void orth_store_kernel(OrthPrepArgs a, void* o
   }
 }
 
+// ---- small matrices: everything in one launch ------------------------------------------------------------------------
+// A workgroup of eight wavefronts takes a matrix of up to SP x LP on its shorter and longer side: X stays in registers in
+// fp32, in the order of the update product's accumulators; in LDS lie its fp16 copy (operand of S = X X^T by rows, of the
+// update by columns through the transposing read) and S, replaced by its polynomial P.  Fifteen products of 128^3 and thirty
+// barriers are what bounds it: the LDS reads of a product take as long as its matrix instructions (1500 cycles).
+// LDS rows of both are multiples of 256 bytes; the sixteen 16-byte chunks of 256 bytes are XOR-swizzled by the row so that
+// neither the 16 rows of a row read nor the eight rows (k & 3, k & 8) of 32 bytes of a transposing read share banks.
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(8))) short s16x8_t;
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+constexpr int SMALL_THREADS = 512;
+
+struct OrthSmallArgs {
+  OrthPrepArgs prep;
+  void* out;
+  OrthSteps steps;
+};
+
+__device__ __forceinline__ int swizzle(int row, int chunk) {
+  return chunk ^ (((row & 3) << 1) | (row & 8) | ((row >> 2) & 1));
+}
+template <int PITCH>
+__device__ __forceinline__ f16x8_t row_fragment(const char* m, int row, int chunk) {
+  return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const s16x8_t*>(m + row * PITCH + (swizzle(row, chunk) << 4)));
+}
+// four fp16 values of row `row` from column `col` (a multiple of 4) on
+template <int PITCH>
+__device__ __forceinline__ void put4(char* m, int row, int col, const float (&x)[4]) {
+  f16x4_t h;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) h[v] = (_Float16)x[v];
+  *reinterpret_cast<f16x4_t*>(m + row * PITCH + (swizzle(row, col >> 3) << 4) + (col & 7) * 2) = h;
+}
+
+template <int SP, int LP, bool BF16G>
+__global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  constexpr int UP = LP + 1;                       // fp32 U in LDS: [SP][UP], before anything else lies there
+  constexpr int XPITCH = LP * 2 < 256 ? 256 : LP * 2, SPITCH = 256;
+  constexpr int FI = LP / 32, FJ = SP / 64, GI = SP / 32;     // 16 x 16 blocks of a wavefront: update, gram and polynomial
+  const OrthPrepArgs& o = a.prep;
+  const gecc_orth_params& p = o.p;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
+  const int wi = wave & 1, wj = wave >> 1;
+  const int b = blockIdx.x;
+  float* U = reinterpret_cast<float*>(smem);
+  double* red = reinterpret_cast<double*>(smem + SP * UP * 4 / 8 * 8 + 8);
+  // G and M once; U by (short side, long side), zeros around it
+  for (int q = tid; q < SP * UP; q += SMALL_THREADS) U[q] = 0.f;
+  __syncthreads();
+  double sum = 0.0;
+  {
+    const int n = p.rows * p.cols;
+    float* M = o.M ? o.M + (int64_t)b * p.stride_m : nullptr;
+    for (int q0 = tid; q0 < n; q0 += 8 * SMALL_THREADS) {
+      float x[8], m[8];
+#pragma unroll
+      for (int h = 0; h < 8; ++h) {
+        const int q = q0 + h * SMALL_THREADS, row = q / p.cols, c = q - row * p.cols;
+        x[h] = m[h] = 0.f;
+        if (q < n) {
+          const int64_t at = (int64_t)b * p.stride_g + row * p.ld_g + c;
+          x[h] = BF16G ? bf16_of(static_cast<const uint16_t*>(o.G)[at]) : static_cast<const float*>(o.G)[at];
+          if (M) m[h] = M[row * p.ld_m + c];
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 8; ++h) {
+        const int q = q0 + h * SMALL_THREADS, row = q / p.cols, c = q - row * p.cols;
+        if (q >= n) break;
+        if (M) {
+          m[h] = fmaf(p.mu, m[h], x[h]);
+          M[row * p.ld_m + c] = m[h];
+          x[h] = update_of(o, x[h], m[h]);
+        }
+        sum = fma((double)x[h], (double)x[h], sum);
+        U[(o.tall ? c : row) * UP + (o.tall ? row : c)] = x[h];
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+  if (lane == 0) red[wave] = sum;
+  __syncthreads();
+  sum = ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
+  const float f = (float)((double)a.steps.sx[0] / (sqrt(sum) + (double)p.eps));
+  // x[i][j][v]: element (short side 16 (FJ wj + j) + l16, long side 16 (FI wi + i) + 4 g + v), times sx
+  float x[FI][FJ][4];
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        x[i][j][v] = f * U[((FJ * wj + j) * 16 + l16) * UP + (FI * wi + i) * 16 + 4 * g + v];
+  __syncthreads();
+  char* X = smem;
+  char* S = smem + SP * XPITCH;
+  const int ksteps_l = (o.l + 31) / 32, ksteps_s = (o.s + 31) / 32;
+  for (int t = 0; t < p.steps; ++t) {
+    const float sx = a.steps.sx[t], ss = a.steps.ss[t], sp = a.steps.sp[t], fold = a.steps.fold[t];
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) put4<XPITCH>(X, (FJ * wj + j) * 16 + l16, (FI * wi + i) * 16 + 4 * g, x[i][j]);
+    __syncthreads();
+    // S (i, j blocks: wi, wj); its row j gets the values of its column j: S is symmetric
+    f32x4_t gram[GI][FJ], poly[GI][FJ];
+#pragma unroll
+    for (int i = 0; i < GI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) gram[i][j] = poly[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < ksteps_l; ++k) {
+      f16x8_t fa[GI], fb[FJ];
+#pragma unroll
+      for (int i = 0; i < GI; ++i) fa[i] = row_fragment<XPITCH>(X, (GI * wi + i) * 16 + l16, k * 4 + g);
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) fb[j] = row_fragment<XPITCH>(X, (FJ * wj + j) * 16 + l16, k * 4 + g);
+#pragma unroll
+      for (int i = 0; i < GI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) gram[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[i], fb[j], gram[i][j], 0, 0, 0);
+    }
+    const float to_s = ss / (sx * sx);
+#pragma unroll
+    for (int i = 0; i < GI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) {
+        float y[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          y[v] = gram[i][j][v] * to_s;
+          gram[i][j][v] = (float)(_Float16)y[v];      // the S that both terms of P are made from
+        }
+        put4<SPITCH>(S, (FJ * wj + j) * 16 + l16, (GI * wi + i) * 16 + 4 * g, y);
+      }
+    __syncthreads();
+    for (int k = 0; k < ksteps_s; ++k) {
+      f16x8_t fa[GI], fb[FJ];
+#pragma unroll
+      for (int i = 0; i < GI; ++i) fa[i] = row_fragment<SPITCH>(S, (GI * wi + i) * 16 + l16, k * 4 + g);
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) fb[j] = row_fragment<SPITCH>(S, (FJ * wj + j) * 16 + l16, k * 4 + g);
+#pragma unroll
+      for (int i = 0; i < GI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) poly[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[i], fb[j], poly[i][j], 0, 0, 0);
+    }
+    __syncthreads();
+    const float of_s = p.b * (sp / ss), of_ss = p.c * (sp / (ss * ss)), eye = fold * p.a * sp;
+#pragma unroll
+    for (int i = 0; i < GI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) {
+        float y[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          y[v] = fmaf(of_s, gram[i][j][v], of_ss * poly[i][j][v]);
+          if ((GI * wi + i) * 16 + 4 * g + v == (FJ * wj + j) * 16 + l16) y[v] += eye;
+        }
+        put4<SPITCH>(S, (FJ * wj + j) * 16 + l16, (GI * wi + i) * 16 + 4 * g, y);
+      }
+    __syncthreads();
+    const bool last = t + 1 == p.steps;
+    const float to = last ? p.scale : a.steps.sx[t + 1], of_x = (1.f - fold) * p.a * (to / sx), of_px = to / (sp * sx);
+    f32x4_t acc[FI][FJ];
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < ksteps_s; ++k) {
+      f16x8_t fb[FJ];
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) fb[j] = row_fragment<SPITCH>(S, (FJ * wj + j) * 16 + l16, k * 4 + g);
+      const int q4 = (lane & 3) * 4, row = k * 32 + 8 * g + ((lane >> 2) & 3);
+#pragma unroll
+      for (int i = 0; i < FI; ++i) {
+        const int col = (FI * wi + i) * 16 + q4;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(X + row * XPITCH + (swizzle(row, col >> 3) << 4) + (col & 7) * 2));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(X + (row + 4) * XPITCH + (swizzle(row + 4, col >> 3) << 4) + (col & 7) * 2));
+        const f16x8_t fa = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa, fb[j], acc[i][j], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[i][j][v] = fmaf(of_x, x[i][j][v], of_px * acc[i][j][v]);
+    __syncthreads();                              // X and S are free again
+  }
+  const float last_f = p.steps == 0 ? p.scale / a.steps.sx[0] : 1.f;
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int is = (FJ * wj + j) * 16 + l16, il = (FI * wi + i) * 16 + 4 * g + v;
+        if (is >= o.s || il >= o.l) continue;
+        const int64_t at = (int64_t)b * p.stride_o + (o.tall ? il * p.ld_o + is : is * p.ld_o + il);
+        const float y = x[i][j][v] * last_f;
+        if (p.out_dtype == GECC_F32) static_cast<float*>(a.out)[at] = y;
+        else static_cast<uint16_t*>(a.out)[at] = to_bf16(y);
+      }
+}
+
+template <int SP, int LP>
+hipError_t small(const OrthSmallArgs& a, hipStream_t st) {
+  constexpr int u_bytes = SP * (LP + 1) * 4 / 8 * 8 + 8 + 64, x_bytes = SP * (LP * 2 < 256 ? 256 : LP * 2) + SP * 256;
+  constexpr int lds = u_bytes > x_bytes ? u_bytes : x_bytes;
+  auto kern = a.prep.p.dtype == GECC_BF16 ? orth_small_kernel<SP, LP, true> : orth_small_kernel<SP, LP, false>;
+  if (lds > 65536) {
+    static LdsLimit limit[2];
+    const hipError_t e = limit[a.prep.p.dtype == GECC_BF16].raise(reinterpret_cast<const void*>(kern), lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kern, dim3(a.prep.p.batch), dim3(SMALL_THREADS), lds, st, a);
+  return hipGetLastError();
+}
+
 bool vectors_ok(const OrthPrepArgs& a) {
   const int64_t es = a.p.dtype == GECC_F32 ? 4 : 2;
   if (reinterpret_cast<uintptr_t>(a.G) % 16 || a.p.ld_g * es % 16 || (a.p.batch > 1 && a.p.stride_g * es % 16)) return false;
@@ -178,6 +418,15 @@ hipError_t launch_orth_start(const OrthPrepArgs& a, hipStream_t st) {
   const bool vec = vectors_ok(a);
   if (a.p.dtype == GECC_BF16) return vec ? start<true, true>(a, st) : start<true, false>(a, st);
   return vec ? start<false, true>(a, st) : start<false, false>(a, st);
+}
+
+bool orth_small_ok(int s, int l) { return s <= 128 && l <= 256; }
+
+hipError_t launch_orth_small(const OrthPrepArgs& prep, void* out, const OrthSteps& steps, hipStream_t st) {
+  if (!orth_small_ok(prep.s, prep.l)) return hipErrorInvalidValue;
+  const OrthSmallArgs a = {prep, out, steps};
+  if (prep.s <= 64) return prep.l <= 128 ? small<64, 128>(a, st) : small<64, 256>(a, st);
+  return prep.l <= 128 ? small<128, 128>(a, st) : small<128, 256>(a, st);
 }
 
 hipError_t launch_orth_store(const OrthPrepArgs& a, void* out, hipStream_t st) {

@@ -16,6 +16,7 @@
 #include "ops_internal.h"
 #include "dma_device.h"
 #include "ops_device.h"
+#include "lds_limit.h"
 
 namespace gecc {
 namespace {
@@ -57,11 +58,19 @@ __device__ __forceinline__ void store4(const TileArgs& a, int b, int i, int j, b
     for (int v = 0; v < 4; ++v) x[v] = a.f_acc * acc[v];
   } else {
     const int64_t at = b * a.s_old + (int64_t)j * a.ld_old + i;
-    const f16x4_t hi = *reinterpret_cast<const f16x4_t*>(a.old_hi + at);
-    f16x4_t lo = {0, 0, 0, 0};
-    if (EPI == EPI_UPDATE && a.old_lo) lo = *reinterpret_cast<const f16x4_t*>(a.old_lo + at);
+    float old[4] = {0.f, 0.f, 0.f, 0.f};
+    if (EPI == EPI_POLY || a.old_hi) {
+      const f16x4_t hi = *reinterpret_cast<const f16x4_t*>(a.old_hi + at);
+      f16x4_t lo = {0, 0, 0, 0};
+      if (EPI == EPI_UPDATE) lo = *reinterpret_cast<const f16x4_t*>(a.old_lo + at);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) x[v] = fmaf(a.f_old, (float)hi[v] + (float)lo[v], a.f_acc * acc[v]);
+      for (int v = 0; v < 4; ++v) old[v] = (float)hi[v] + (float)lo[v];
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      x[v] = fmaf(a.f_old, old[v], a.f_acc * acc[v]);
+      if (EPI == EPI_POLY && i + v == j) x[v] += a.f_eye;
+    }
   }
   if (EPI == EPI_UPDATE && a.last) {
     // (no loops over the four with a run-time end: the caller's rows and columns end anywhere)
@@ -96,7 +105,7 @@ __device__ __forceinline__ void store4(const TileArgs& a, int b, int i, int j, b
 }
 
 // ---- operands --------------------------------------------------------------------------------------------------------
-// KC: k-contiguous.  Otherwise (T rows = 128, fp16): element (row, k) at P[k * ld + row].
+// KC: k-contiguous.  Otherwise (fp16): element (row, k) at P[k * ld + row].
 template <bool KC, int T>
 struct TileOperand {
   static constexpr int NV = T * 128 / (THREADS * 16);     // DMA instructions of a wavefront per stage
@@ -106,6 +115,12 @@ struct TileOperand {
   unsigned voff[NV];
   int frag[T / 32];
 
+  // place of 16-byte unit p of k-row `krow` in the LDS row (and the other way round): a transposing read takes 32 bytes of
+  // eight rows (k & 3, k & 8) in one cycle, which have to lie in different banks (rows are 256 or 128 bytes long)
+  static __device__ __forceinline__ int unit(int krow, int p) {
+    if (T == 128) return p ^ ((krow & 3) << 2) ^ (((krow >> 3) & 1) << 1);
+    return p ^ (((krow >> 1) & 1) << 1) ^ (((krow >> 3) & 1) << 2);
+  }
   __device__ __forceinline__ void init(const uint8_t* P, int64_t ld, int r0, int rows, int cols, int stage0, int sub) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
     if (KC) {
@@ -128,15 +143,14 @@ struct TileOperand {
       left = (int64_t)(rows - stage0 * 64) * ld - (int64_t)r0 * 2;      // (rows: the valid k)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int s = (wave * NV + i) * 64 + lane, krow = s >> 4, p = s & 15;
-        const int u = (((p >> 2) ^ (krow & 3)) << 2) | ((p & 3) ^ (((krow >> 3) & 1) << 1));
+        const int s = (wave * NV + i) * 64 + lane, krow = s / (T / 8), u = unit(krow, s % (T / 8));
         voff[i] = r0 + u * 8 < cols ? (unsigned)(krow * ld + u * 16) : OOB;
       }
       const int j = (lane >> 2) & 3, q = lane & 3;
 #pragma unroll
       for (int i = 0; i < T / 32; ++i) {
-        const int col = sub + i * 16 + 4 * q, krow = 8 * g + j, u = col >> 3;
-        frag[i] = krow * 256 + (((((u >> 2) ^ j) << 2) | ((u & 3) ^ ((g & 1) << 1))) << 4) + (col & 7) * 2;
+        const int col = sub + i * 16 + 4 * q, krow = 8 * g + j;
+        frag[i] = krow * (T * 2) + (unit(krow, col >> 3) << 4) + (col & 7) * 2;
       }
     }
   }
@@ -150,9 +164,9 @@ struct TileOperand {
   // the 16 bytes a lane of fragment i (16 rows), instruction ks (0, 1) of the stage
   __device__ __forceinline__ s16x8_t fragment(const char* region, int i, int ks) const {
     if (KC) return *reinterpret_cast<const s16x8_t*>(region + (frag[i] ^ (ks << 6)));
-    const char* p = region + frag[i] + ks * 32 * 256;
+    const char* p = region + frag[i] + ks * 32 * (T * 2);
     const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(p));
-    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(p + 4 * 256));
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(p + 4 * (T * 2)));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 };
@@ -173,7 +187,8 @@ __device__ __forceinline__ void tile_at(const TileArgs& a, int t, int& tm, int& 
   tn = t / ntm;
 }
 
-template <int KIND, bool KCA, int T, int EPI>
+// RING: stages of LDS, RING - 1 of them on their way while one is in use
+template <int KIND, bool KCA, int T, int RING, int EPI>
 __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_out) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int F = T / 32;                       // 16-row fragments of a wavefront, an operand
@@ -222,11 +237,11 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
 
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   auto issue = [&](int t) {
-    const unsigned at = lds0 + (t & 1) * SLOT;
+    const unsigned at = lds0 + (t & (RING - 1)) * SLOT;
     if (KIND == KIND_MX4 && (t & 1) == 0) {
       const int64_t off = (int64_t)(t >> 1) * 256, rest = sleft - off;
       const i32x4_t rsrc = make_rsrc(sbase + off, rest <= 0 ? 0u : rest > 0x7fffffff ? 0x7fffffffu : (unsigned)rest);
-      dma16(lds0 + 2 * SLOT + ((t >> 1) & 1) * 2 * SCALES + slds, svoff, rsrc, 0);
+      dma16(lds0 + RING * SLOT + ((t >> 1) & (RING / 2 - 1)) * 2 * SCALES + slds, svoff, rsrc, 0);
     }
     oa.issue(at, wave_u, t);
     ob.issue(at + STAGE, wave_u, t);
@@ -236,10 +251,10 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
   for (int i = 0; i < F; ++i) sa[i] = sb[i] = 0;
   auto multiply = [&](int t, auto odd_c) {
     constexpr bool ODD = decltype(odd_c)::value;
-    const char* ra = smem + (ODD ? SLOT : 0);
+    const char* ra = smem + (t & (RING - 1)) * SLOT;
     const char* rb = ra + STAGE;
     if (KIND == KIND_MX4 && !ODD) {
-      const char* rs = smem + 2 * SLOT + ((t >> 1) & 1) * 2 * SCALES;
+      const char* rs = smem + RING * SLOT + ((t >> 1) & (RING / 2 - 1)) * 2 * SCALES;
 #pragma unroll
       for (int i = 0; i < F; ++i) {
         sa[i] = *reinterpret_cast<const int*>(rs + (wr * (T / 2) + i * 16 + l16) * 16 + g * 4);
@@ -269,15 +284,20 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
         }
     }
   };
+  // Stage t has landed when no more instructions are pending than the stages behind it have (a stage's scales go out first)
+  constexpr int PER = TileOperand<KCA, T>::NV + TileOperand<true, T>::NV;
   auto step = [&](int t, auto odd_c) {
-    wait_vm<0>();                                        // stage t of this wavefront's loads
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // its reads of stage t - 1 are back
-    __builtin_amdgcn_s_barrier();                        // stage t complete for everyone, the other slot free
+    const int behind = min(RING - 2, count - 1 - t);
+    if (RING > 3 && behind == 2) wait_vm<(RING > 3 ? 2 : 0) * PER>();
+    else if (RING > 2 && behind == 1) wait_vm<(RING > 2 ? 1 : 0) * PER>();
+    else wait_vm<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wavefront's reads of stage t - 1 are back
+    __builtin_amdgcn_s_barrier();                        // stage t complete for everyone, the slot of stage t - 1 free
     asm volatile("" ::: "memory");
-    if (t + 1 < count) issue(t + 1);
+    if (t + RING - 1 < count) issue(t + RING - 1);
     multiply(t, odd_c);
   };
-  issue(0);
+  for (int t = 0; t < min(RING - 1, count); ++t) issue(t);
   for (int t = 0; t < count; t += 2) {
     step(t, std::false_type{});
     if (t + 1 < count) step(t + 1, std::true_type{});
@@ -327,8 +347,9 @@ int64_t tiles_of(int64_t m_rows, int64_t n_rows, int T, bool symmetric) {
   return symmetric ? tm * (tm + 1) / 2 : tm * tn;
 }
 
-template <int KIND, bool KCA, int T, int EPI>
+template <int KIND, bool KCA, int T, int RING, int EPI>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
+  static_assert(RING == 2 || RING == 4, "the waits of tile_kernel");
   const int64_t tiles = tiles_of(a.m_rows, a.n_rows, T, a.symmetric);
   if (tiles > 0x7fffffff || a.batch > 65535) return hipErrorInvalidValue;
   bool vec = false;
@@ -336,10 +357,11 @@ hipError_t launch(const TileArgs& a, hipStream_t st) {
     const int es = a.out_dtype == GECC_F32 ? 4 : 2;
     vec = reinterpret_cast<uintptr_t>(a.out) % (4 * es) == 0 && a.ldo % 4 == 0 && a.so % 4 == 0;
   }
-  constexpr int lds = 2 * 2 * T * 128 + (KIND == KIND_MX4 ? 2 * 2 * T * 16 : 0);
-  auto kern = tile_kernel<KIND, KCA, T, EPI>;
+  constexpr int lds = RING * 2 * T * 128 + (KIND == KIND_MX4 ? RING / 2 * 2 * T * 16 : 0);
+  auto kern = tile_kernel<KIND, KCA, T, RING, EPI>;
   if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static LdsLimit limit;
+    const hipError_t e = limit.raise(reinterpret_cast<const void*>(kern), lds);
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(kern, dim3((unsigned)tiles, a.split, a.batch), dim3(THREADS), lds, st, a, vec);
@@ -354,8 +376,8 @@ hipError_t launch(const TileArgs& a, hipStream_t st) {
 
 TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, int stages, int batch, bool symmetric) {
   TilePlan p;
-  // 128 x 128 tiles once they fill the chip; A with its rows contiguous has no others
-  p.tile = epi == EPI_UPDATE || tiles_of(m_rows, n_rows, 128, symmetric) * batch >= 256 ? 128 : 64;
+  // 128 x 128 tiles once they fill the chip
+  p.tile = tiles_of(m_rows, n_rows, 128, symmetric) * batch >= 256 ? 128 : 64;
   const int64_t tiles = tiles_of(m_rows, n_rows, p.tile, symmetric) * batch;
   const int pairs = (stages + 1) / 2;
   int64_t s = 512 / tiles;
@@ -363,20 +385,26 @@ TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, 
   if (s > pairs / 2) s = pairs / 2;
   p.split = s < 1 ? 1 : (int)s;
   p.part_bytes = p.split > 1 ? (size_t)tiles * p.split * p.tile * p.tile * 4 : 0;
-  (void)kind;
+  (void)kind; (void)epi;
   return p;
 }
+
+namespace {
+template <int KIND, bool KCA, int EPI>
+hipError_t launch_any(const TileArgs& a, const TilePlan& plan, hipStream_t st) {
+  // (64 KiB of LDS either way, two workgroups a compute unit)
+  return plan.tile == 128 ? launch<KIND, KCA, 128, 2, EPI>(a, st) : launch<KIND, KCA, 64, 4, EPI>(a, st);
+}
+}  // namespace
 
 hipError_t launch_tiles(TileKind kind, TileEpi epi, const TileArgs& a0, const TilePlan& plan, hipStream_t st) {
   TileArgs a = a0;
   a.split = plan.split;
-  if (kind == KIND_MX4) {
-    return plan.tile == 128 ? launch<KIND_MX4, true, 128, EPI_OUT>(a, st) : launch<KIND_MX4, true, 64, EPI_OUT>(a, st);
-  }
+  if (kind == KIND_MX4) return launch_any<KIND_MX4, true, EPI_OUT>(a, plan, st);
   switch (epi) {
-    case EPI_GRAM: return plan.tile == 128 ? launch<KIND_F16, true, 128, EPI_GRAM>(a, st) : launch<KIND_F16, true, 64, EPI_GRAM>(a, st);
-    case EPI_POLY: return plan.tile == 128 ? launch<KIND_F16, true, 128, EPI_POLY>(a, st) : launch<KIND_F16, true, 64, EPI_POLY>(a, st);
-    case EPI_UPDATE: return launch<KIND_F16, false, 128, EPI_UPDATE>(a, st);
+    case EPI_GRAM: return launch_any<KIND_F16, true, EPI_GRAM>(a, plan, st);
+    case EPI_POLY: return launch_any<KIND_F16, true, EPI_POLY>(a, plan, st);
+    case EPI_UPDATE: return launch_any<KIND_F16, false, EPI_UPDATE>(a, plan, st);
     default: return hipErrorInvalidValue;
   }
 }

@@ -6,6 +6,7 @@ Outputs and workspaces come from torch's allocator, which keeps their memory in 
 There is no CPU fallback.
 """
 import ctypes as C
+import functools
 from typing import Optional, Tuple
 
 import torch
@@ -78,19 +79,26 @@ def _ld(t):
 
 def _output(out, shape, dtype, device, what):
     if out is None:
+        if dtype not in _DTYPES:
+            raise GeccError("%s: %s is not supported (float32 and bfloat16 are)" % (what, dtype))
         return torch.empty(shape, dtype=dtype, device=device)
-    if out.device != device or tuple(out.shape) != tuple(shape) or out.dtype not in _DTYPES or out.data_ptr() != _rows(out).data_ptr():
+    if out.device != device or tuple(out.shape) != tuple(shape) or out.dtype not in _DTYPES or _rows(out) is not out:
         raise GeccError("%s: out has to be a float32 or bfloat16 tensor of shape %s with contiguous rows on %s" % (what, tuple(shape), device))
     return out
 
 
+# (sizes alone: the library's functions of the shape, asked once a shape)
+@functools.lru_cache(maxsize=4096)
+def _bytes(name, *shape):
+    return getattr(lib(), name)(*shape)
+
+
 def _workspace(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-
-
-def _aligned(ws):
-    # (torch's allocator hands out multiples of 512 bytes)
-    return _ptr(ws), 0 if ws is None else ws.numel()
+    """(tensor or None, its address, its size); torch's allocator hands out multiples of 512 bytes."""
+    if not nbytes:
+        return None, 0, 0
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), nbytes
 
 
 class Mx4:
@@ -98,32 +106,48 @@ class Mx4:
     the layout of include/gecc_ops.h."""
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
-        self.data, self.scales, self.rows, self.cols = data, scales, int(rows), int(cols)
+        self.rows, self.cols = int(rows), int(cols)
         for t, f, what in ((data, "gecc_mx4_data_bytes", "data"), (scales, "gecc_mx4_scale_bytes", "scales")):
             if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous():
                 raise GeccError("Mx4: %s has to be a contiguous uint8 tensor on the GPU" % what)
-            need = getattr(lib(), f)(self.rows, self.cols)
+            need = _bytes(f, self.rows, self.cols)
             if need == 0 or t.numel() != need:
                 raise GeccError("Mx4: %s of a %d x %d matrix has %d bytes, got %d" % (what, rows, cols, need, t.numel()))
         if data.device != scales.device:
             raise GeccError("Mx4: data and scales are on different devices")
+        self._kept, self.device = (data, scales), data.device
+        self._data, self._scales = data.data_ptr(), scales.data_ptr()
+
+    @classmethod
+    def _new(cls, rows, cols, device):
+        """An empty one, both buffers in one allocation."""
+        q = cls.__new__(cls)
+        n = _bytes("gecc_mx4_data_bytes", rows, cols)
+        if n == 0:
+            raise GeccError("mx4: a matrix of %d x %d" % (rows, cols))
+        both = torch.empty(n + _bytes("gecc_mx4_scale_bytes", rows, cols), dtype=torch.uint8, device=device)
+        q.rows, q.cols, q.device, q._kept = rows, cols, both.device, both
+        q._data = both.data_ptr()
+        q._scales = q._data + n         # (n is a multiple of 128)
+        return q
+
+    def _parts(self):
+        if not isinstance(self._kept, tuple):
+            n = self._scales - self._data
+            self._kept = (self._kept[:n], self._kept[n:])
+        return self._kept
+
+    @property
+    def data(self):
+        return self._parts()[0]
+
+    @property
+    def scales(self):
+        return self._parts()[1]
 
     @property
     def shape(self):
         return self.rows, self.cols
-
-    @property
-    def device(self):
-        return self.data.device
-
-
-def _new_mx4(rows, cols, device):
-    L = lib()
-    q = Mx4.__new__(Mx4)
-    q.rows, q.cols = rows, cols
-    q.data = torch.empty(L.gecc_mx4_data_bytes(rows, cols), dtype=torch.uint8, device=device)
-    q.scales = torch.empty(L.gecc_mx4_scale_bytes(rows, cols), dtype=torch.uint8, device=device)
-    return q
 
 
 def _mx4(q, what):
@@ -132,12 +156,16 @@ def _mx4(q, what):
     return q
 
 
-def _one_device(what, *ts):
-    d = ts[0].device
-    if any(t is not None and t.device != d for t in ts):
-        raise GeccError("%s: operands on different devices" % what)
-    if d.index != torch.cuda.current_device():
-        raise GeccError("%s: operands are on %s, the current device is cuda:%d" % (what, d, torch.cuda.current_device()))
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _one_device(what, first, *others):
+    d = first.device
+    for t in others:
+        if t is not None and t.device != d:
+            raise GeccError("%s: operands on different devices" % what)
+    if d.index != _current_device():
+        raise GeccError("%s: operands are on %s, the current device is cuda:%d" % (what, d, _current_device()))
     return d
 
 
@@ -147,21 +175,18 @@ def mx4_quantize(x: torch.Tensor, both: bool = False):
     x = _matrix(x, "mx4_quantize")
     d = _one_device("mx4_quantize", x)
     rows, cols = x.shape
-    q = _new_mx4(rows, cols, d)
-    t = _new_mx4(cols, rows, d) if both else None
-    _check(lib().gecc_mx4_quantize(_ptr(x), _DTYPES[x.dtype], rows, cols, _ld(x), _ptr(q.data), _ptr(q.scales),
-                                   _ptr(t.data) if both else 0, _ptr(t.scales) if both else 0, _stream()))
+    q = Mx4._new(rows, cols, d)
+    t = Mx4._new(cols, rows, d) if both else None
+    _check(lib().gecc_mx4_quantize(x.data_ptr(), _DTYPES[x.dtype], rows, cols, _ld(x), q._data, q._scales, t._data if both else 0,
+                                   t._scales if both else 0, _stream()))
     return (q, t) if both else q
 
 
 def mx4_dequantize(q: Mx4, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values of an Mx4 matrix (exact in both types)."""
     _mx4(q, "mx4_dequantize")
-    d = _one_device("mx4_dequantize", q)
-    out = _output(out, q.shape, dtype, d, "mx4_dequantize")
-    if out.dtype not in _DTYPES:
-        raise GeccError("mx4_dequantize: %s is not supported" % out.dtype)
-    _check(lib().gecc_mx4_dequantize(_ptr(q.data), _ptr(q.scales), q.rows, q.cols, _ptr(out), _DTYPES[out.dtype], _ld(out), _stream()))
+    out = _output(out, q.shape, dtype, _one_device("mx4_dequantize", q), "mx4_dequantize")
+    _check(lib().gecc_mx4_dequantize(q._data, q._scales, q.rows, q.cols, out.data_ptr(), _DTYPES[out.dtype], _ld(out), _stream()))
     return out
 
 
@@ -173,11 +198,8 @@ def mx4_gemm(a: Mx4, b: Mx4, dtype=torch.float32, out: Optional[torch.Tensor] = 
     d = _one_device("mx4_gemm", a, b)
     n, k, m = a.rows, a.cols, b.rows
     out = _output(out, (n, m), dtype, d, "mx4_gemm")
-    if out.dtype not in _DTYPES:
-        raise GeccError("mx4_gemm: %s is not supported" % out.dtype)
-    ws = _workspace(lib().gecc_mx4_gemm_workspace(n, k, m), d)
-    _check(lib().gecc_mx4_gemm(n, k, m, _ptr(a.data), _ptr(a.scales), _ptr(b.data), _ptr(b.scales), _ptr(out), _DTYPES[out.dtype], _ld(out),
-                               *_aligned(ws), _stream()))
+    ws, at, size = _workspace(_bytes("gecc_mx4_gemm_workspace", n, k, m), d)
+    _check(lib().gecc_mx4_gemm(n, k, m, a._data, a._scales, b._data, b._scales, out.data_ptr(), _DTYPES[out.dtype], _ld(out), at, size, _stream()))
     return out
 
 
@@ -185,18 +207,16 @@ def mx4_linear(x: torch.Tensor, w: Mx4, dtype=None, out: Optional[torch.Tensor] 
     """Q(x) w^T: tokens (n x k, float32 or bfloat16, quantised on the way) through a layer whose weight (m x k) is kept in 4
     bits; n x m of `dtype` (x's own by default).  No tokens: an empty result."""
     x, _ = _matrix(x, "mx4_linear"), _mx4(w, "mx4_linear")
-    if x.shape[1] != w.cols:
-        raise GeccError("mx4_linear: tokens of %d values against a weight of %d columns" % (x.shape[1], w.cols))
-    d = _one_device("mx4_linear", x, w)
     n, k, m = x.shape[0], w.cols, w.rows
+    if x.shape[1] != k:
+        raise GeccError("mx4_linear: tokens of %d values against a weight of %d columns" % (x.shape[1], k))
+    d = _one_device("mx4_linear", x, w)
     out = _output(out, (n, m), x.dtype if dtype is None else dtype, d, "mx4_linear")
-    if out.dtype not in _DTYPES:
-        raise GeccError("mx4_linear: %s is not supported" % out.dtype)
     if n == 0:
         return out
-    ws = _workspace(lib().gecc_mx4_linear_workspace(n, k, m), d)
-    _check(lib().gecc_mx4_linear(n, k, m, _ptr(x), _DTYPES[x.dtype], _ld(x), _ptr(w.data), _ptr(w.scales), _ptr(out), _DTYPES[out.dtype],
-                                 _ld(out), *_aligned(ws), _stream()))
+    ws, at, size = _workspace(_bytes("gecc_mx4_linear_workspace", n, k, m), d)
+    _check(lib().gecc_mx4_linear(n, k, m, x.data_ptr(), _DTYPES[x.dtype], _ld(x), w._data, w._scales, out.data_ptr(), _DTYPES[out.dtype],
+                                 _ld(out), at, size, _stream()))
     return out
 
 
@@ -220,10 +240,10 @@ def mx4_linear_backward(dy: torch.Tensor, wt: Optional[Mx4], xt: Optional[Mx4], 
         raise GeccError("mx4_linear_backward: %s is not supported" % dtype)
     dx = torch.empty((n, k), dtype=dtype, device=d) if wt is not None else None
     dw = torch.empty((m, k), dtype=torch.float32, device=d) if xt is not None else None
-    ws = _workspace(lib().gecc_mx4_linear_backward_workspace(n, k, m), d)
-    _check(lib().gecc_mx4_linear_backward(n, k, m, _ptr(dy), _DTYPES[dy.dtype], _ld(dy), _ptr(wt and wt.data), _ptr(wt and wt.scales),
-                                          _ptr(xt and xt.data), _ptr(xt and xt.scales), _ptr(dx), _DTYPES[dtype], k, _ptr(dw), k,
-                                          *_aligned(ws), _stream()))
+    ws, at, size = _workspace(_bytes("gecc_mx4_linear_backward_workspace", n, k, m), d)
+    _check(lib().gecc_mx4_linear_backward(n, k, m, dy.data_ptr(), _DTYPES[dy.dtype], _ld(dy), wt._data if wt else 0, wt._scales if wt else 0,
+                                          xt._data if xt else 0, xt._scales if xt else 0, _ptr(dx), _DTYPES[dtype], k, _ptr(dw), k, at, size,
+                                          _stream()))
     return dx, dw
 
 
@@ -242,8 +262,6 @@ def orthogonalize(g: torch.Tensor, momentum: Optional[torch.Tensor] = None, mu: 
     if momentum is not None and (momentum.dtype != torch.float32 or momentum.shape != g.shape or _rows(momentum) is not momentum):
         raise GeccError("orthogonalize: the momentum has to be a float32 tensor of g's shape with contiguous rows")
     out = _output(out, g.shape, dtype, d, "orthogonalize")
-    if out.dtype not in _DTYPES:
-        raise GeccError("orthogonalize: %s is not supported" % out.dtype)
     rows, cols = g.shape[-2:]
     batch = g.shape[0] if g.dim() == 3 else 1
 
@@ -253,7 +271,7 @@ def orthogonalize(g: torch.Tensor, momentum: Optional[torch.Tensor] = None, mu: 
                    nesterov=1 if nesterov else 0, reserved=0, ld_g=_ld(g), ld_m=_ld(momentum) if momentum is not None else 0, ld_o=_ld(out),
                    stride_g=stride(g), stride_m=stride(momentum), stride_o=stride(out), mu=mu, eps=eps, scale=scale,
                    a=coefficients[0], b=coefficients[1], c=coefficients[2])
-    nbytes = lib().gecc_orthogonalize_workspace(C.byref(p))
-    ws = _workspace(nbytes, d)
-    _check(lib().gecc_orthogonalize(C.byref(p), _ptr(g), _ptr(momentum), _ptr(out), *_aligned(ws), _stream()))
+    ref = C.byref(p)
+    ws, at, size = _workspace(lib().gecc_orthogonalize_workspace(ref), d)
+    _check(lib().gecc_orthogonalize(ref, g.data_ptr(), _ptr(momentum), out.data_ptr(), at, size, _stream()))
     return out

@@ -104,7 +104,7 @@ def test_products_refuse(ops):
 
 
 def _orth(ops, **kw):
-    d = dict(rows=64, cols=100, batch=1, dtype=0, out_dtype=1, steps=5, nesterov=1, reserved=0, ld_g=100, ld_m=100, ld_o=100, stride_g=0,
+    d = dict(rows=160, cols=300, batch=1, dtype=0, out_dtype=1, steps=5, nesterov=1, reserved=0, ld_g=300, ld_m=300, ld_o=300, stride_g=0,
              stride_m=0, stride_o=0, mu=0.95, eps=1e-7, scale=1.0, a=3.4445, b=-4.775, c=2.0315)
     d.update(kw)
     return ops.OrthParams(**d)
@@ -115,6 +115,8 @@ def test_orthogonalize_refuses(ops):
     p = _orth(ops)
     need = L.gecc_orthogonalize_workspace(C.byref(p))
     assert need > 0
+    small = _orth(ops, rows=128, cols=256, ld_g=256, ld_m=256, ld_o=256)
+    assert L.gecc_orthogonalize_workspace(C.byref(small)) == 0      # (one launch, no workspace)
     nan, inf = float("nan"), float("inf")
     for bad in (dict(rows=0), dict(cols=-1), dict(batch=0), dict(batch=65536), dict(dtype=2), dict(out_dtype=-1), dict(steps=-1), dict(steps=17),
                 dict(nesterov=2), dict(reserved=1), dict(mu=nan), dict(eps=0.0), dict(eps=inf), dict(scale=inf), dict(a=nan), dict(b=inf),
@@ -122,7 +124,7 @@ def test_orthogonalize_refuses(ops):
         q = _orth(ops, **bad)
         assert L.gecc_orthogonalize_workspace(C.byref(q)) == 0, bad
         assert L.gecc_orthogonalize(C.byref(q), OK, OK, OK, OK, need, None) == ARG, bad
-    for bad in (dict(ld_g=99), dict(ld_m=99), dict(ld_o=99), dict(batch=2), dict(batch=2, stride_g=6400, stride_o=6400, stride_m=6399)):
+    for bad in (dict(ld_g=299), dict(ld_m=299), dict(ld_o=299), dict(batch=2), dict(batch=2, stride_g=48000, stride_o=48000, stride_m=47999)):
         q = _orth(ops, **bad)
         assert L.gecc_orthogonalize(C.byref(q), OK, OK, OK, OK, 1 << 30, None) == ARG, bad
     assert L.gecc_orthogonalize(None, OK, OK, OK, OK, need, None) == ARG

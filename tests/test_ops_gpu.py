@@ -65,7 +65,7 @@ def test_quantised_bytes(rows, cols, kind, dtype):
 def test_only_the_transpose_through_the_c_abi():
     x, t = _store(_matrix(_rng(1), 70, 300), "f32")
     want = ops.mx4_quantize(t, both=True)[1]
-    got = ops._new_mx4(300, 70, t.device)
+    got = ops.Mx4._new(300, 70, t.device)
     gecc._check(ops.lib().gecc_mx4_quantize(t.data_ptr(), 0, 70, 300, 300, 0, 0, got.data.data_ptr(), got.scales.data_ptr(), gecc._stream()))
     assert torch.equal(got.data, want.data) and torch.equal(got.scales, want.scales)
 
