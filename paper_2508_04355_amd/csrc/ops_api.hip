@@ -28,7 +28,7 @@ int mx_stages(int64_t k) { return (int)(mx_pad(k) / MX_PAD); }
 
 // ---- C[n x m] = A[n x k] B[m x k]^T ------------------------------------------------------------------
 TilePlan product_plan(int32_t n, int32_t k, int32_t m) {
-  return plan_tiles(KIND_MX4, EPI_OUT, m, n, mx_stages(k), 1, false);
+  return plan_tiles(KIND_MX4, EPI_OUT, m, n, mx_stages(k), 1, false, tile256_ok(mx_pad(k) / 2, 0));
 }
 size_t product_workspace(int32_t n, int32_t k, int32_t m) {
   return n <= MX_FEW_ROWS ? 0 : align_up(product_plan(n, k, m).part_bytes, 256);
@@ -79,11 +79,13 @@ BackwardLayout backward_layout(int32_t n, int32_t k, int32_t m) {
 }
 
 // ---- the orthogonalised update ------------------------------------------------------------------------
+constexpr int64_t ORTH_CHUNK_BYTES = (int64_t)192 << 20;
 struct OrthPlan {
   int s, l;
   bool tall;
   int64_t sp, lp;                 // padded to 64
   int nparts;
+  int chunk;                      // batch items that go through all steps together
   TilePlan gram, poly, update;
   size_t parts, x[2], lo[2], gram_at, poly_at, part, total;
   OrthSteps steps;
@@ -109,16 +111,28 @@ float power_for(double most) {
 bool orth_steps(const gecc_orth_params& p, OrthSteps* o) {
   double sig = 1.0;
   for (int t = 0; t < p.steps; ++t) {
-    sig *= 1.0 + 0x1p-6;          // rounding, and maxima between the points
+    sig *= 1.0 + 0x1p-6;          // rounding
     o->fold[t] = t + 1 == p.steps ? 1.f : t + 2 == p.steps ? 0.5f : 0.f;
     o->sx[t] = power_for(sig);
     o->ss[t] = power_for(sig * sig);
+    // b y + c y^2 + fold a and x (a + b x^2 + c x^4) over y = x^2 in [0, sig^2]: at the ends and where their slopes vanish
+    const double a = p.a, b = p.b, c = p.c, top = sig * sig;
     double next = 0.0, poly = 0.0;
-    for (int i = 0; i <= 2048; ++i) {
-      const double x = sig * i / 2048, y = x * x, q = (double)p.b * y + (double)p.c * y * y;
-      poly = std::fmax(poly, std::fabs(q + o->fold[t] * (double)p.a));
-      next = std::fmax(next, std::fabs(x * ((double)p.a + q)));
+    auto at = [&](double y) {
+      if (!(y >= 0.0 && y <= top)) return;
+      const double q = b * y + c * y * y;
+      poly = std::fmax(poly, std::fabs(q + o->fold[t] * a));
+      next = std::fmax(next, std::sqrt(y) * std::fabs(a + q));
+    };
+    at(0.0);
+    at(top);
+    at(-b / (2.0 * c));                                              // b + 2 c y = 0
+    const double d = 9.0 * b * b - 20.0 * a * c;                     // a + 3 b y + 5 c y^2 = 0
+    if (d >= 0.0) {
+      at((-3.0 * b + std::sqrt(d)) / (10.0 * c));
+      at((-3.0 * b - std::sqrt(d)) / (10.0 * c));
     }
+    at(-a / (3.0 * b));                                              // (c = 0)
     o->sp[t] = power_for(poly * (1.0 + 0x1p-6));
     if (!(next <= 16.0) || !(poly <= 4096.0)) return false;
     sig = next;
@@ -145,12 +159,17 @@ bool orth_plan(const gecc_orth_params* p, OrthPlan* o) {
   o->nparts = (int)(parts > most ? most : parts);
   o->total = 0;
   if (orth_small_ok(o->s, o->l)) return true;
-  o->gram = plan_tiles(KIND_F16, EPI_GRAM, o->s, o->s, (int)(o->lp / 64), p->batch, true);
-  o->poly = plan_tiles(KIND_F16, EPI_POLY, o->s, o->s, (int)(o->sp / 64), p->batch, true);
-  o->update = plan_tiles(KIND_F16, EPI_UPDATE, o->l, o->s, (int)(o->sp / 64), p->batch, false);
+  // X in its two halves, twice, S and P of the items of a chunk: what the steps read and write stays in the 256 MiB memory-side
+  // cache (512 x 512 bf16, 256 items: 3673 us all at once, 2287 in chunks of 64 together with the epilogue by rows)
+  const int64_t item = 4 * o->sp * o->lp * 2 + 2 * (int64_t)o->s * o->sp * 2;
+  const int64_t fit = ORTH_CHUNK_BYTES / item;
+  o->chunk = fit < 1 ? 1 : fit > p->batch ? p->batch : (int)fit;
+  o->gram = plan_tiles(KIND_F16, EPI_GRAM, o->s, o->s, (int)(o->lp / 64), o->chunk, true, tile256_ok(o->lp * 2, 0));
+  o->poly = plan_tiles(KIND_F16, EPI_POLY, o->s, o->s, (int)(o->sp / 64), o->chunk, true, true);
+  o->update = plan_tiles(KIND_F16, EPI_UPDATE, o->l, o->s, (int)(o->sp / 64), o->chunk, false, tile256_ok(o->lp * 2, o->sp));
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
-  const size_t x = (size_t)p->batch * o->s * o->lp * 2, q = (size_t)p->batch * o->s * o->sp * 2;
+  const size_t x = (size_t)o->chunk * o->sp * o->lp * 2, q = (size_t)o->chunk * o->s * o->sp * 2;
   o->parts = take((size_t)p->batch * o->nparts * sizeof(double));
   if (p->steps > 0) {
     o->x[0] = take(x); o->lo[0] = take(x); o->x[1] = take(x); o->lo[1] = take(x);
@@ -163,6 +182,86 @@ bool orth_plan(const gecc_orth_params* p, OrthPlan* o) {
   }
   o->total = off;
   return true;
+}
+
+// items first .. first + items - 1 through all steps, after the norms of all of them
+hipError_t orth_chunk(const gecc_orth_params& params, const OrthPlan& o, OrthPrepArgs prep, void* dev_O, char* ws, int first, int items, hipStream_t st) {
+  const gecc_orth_params* p = &params;
+  auto half = [&](size_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
+  prep.p.batch = items;
+  prep.G = static_cast<const char*>(prep.G) + first * p->stride_g * (int64_t)elem_size(p->dtype);
+  if (prep.M) prep.M += first * p->stride_m;
+  prep.parts += (int64_t)first * prep.nparts;
+  prep.hi = half(o.x[0]);
+  prep.lo = half(o.lo[0]);
+  hipError_t e = launch_orth_start(prep, st);
+  dev_O = static_cast<char*>(dev_O) + first * p->stride_o * (int64_t)elem_size(p->out_dtype);
+
+  const int64_t xs = o.sp * o.lp, qs = (int64_t)o.s * o.sp;     // elements of X, of S and P
+  for (int t = 0; t < p->steps && e == hipSuccess; ++t) {
+    const int cur = t & 1;
+    const bool last = t + 1 == p->steps;
+    const float sx = o.steps.sx[t], ss = o.steps.ss[t], sp = o.steps.sp[t], fold = o.steps.fold[t];
+    TileArgs g{};
+    g.A = g.B = reinterpret_cast<const uint8_t*>(half(o.x[cur]));
+    g.lda = g.ldb = o.lp * 2;
+    g.sa = g.sb = xs * 2;
+    g.m_rows = g.n_rows = o.s;
+    g.stages = (int)(o.lp / 64);
+    g.batch = items;
+    g.part = reinterpret_cast<float*>(ws + o.part);
+    g.out = half(o.gram_at);
+    g.ldo = o.sp; g.so = qs;
+    g.m_store = (int)o.sp; g.n_store = o.s;
+    g.f_acc = ss / (sx * sx);
+    e = launch_tiles(KIND_F16, EPI_GRAM, g, o.gram, st);
+    if (e != hipSuccess) break;
+    TileArgs q = g;
+    q.A = q.B = reinterpret_cast<const uint8_t*>(half(o.gram_at));
+    q.lda = q.ldb = o.sp * 2;
+    q.sa = q.sb = qs * 2;
+    q.stages = (int)(o.sp / 64);
+    q.out = half(o.poly_at);
+    q.old_hi = half(o.gram_at);
+    q.ld_old = o.sp; q.s_old = qs;
+    q.f_old = (float)((double)p->b * sp / ss);
+    q.f_acc = (float)((double)p->c * sp / ((double)ss * ss));
+    q.f_eye = fold * p->a * sp;
+    e = launch_tiles(KIND_F16, EPI_POLY, q, o.poly, st);
+    if (e != hipSuccess) break;
+    TileArgs u{};
+    u.A = reinterpret_cast<const uint8_t*>(half(o.x[cur]));
+    u.lda = o.lp * 2; u.sa = xs * 2;
+    u.a_cols = (int)o.lp; u.k_rows = (int)o.sp;
+    u.B = reinterpret_cast<const uint8_t*>(half(o.poly_at));
+    u.ldb = o.sp * 2; u.sb = qs * 2;
+    u.m_rows = o.l; u.n_rows = o.s;
+    u.stages = (int)(o.sp / 64);
+    u.batch = items;
+    u.part = g.part;
+    if (fold < 1.f) {           // (in the last step all of a X is in P: it needs no second half of X)
+      u.old_hi = half(o.x[cur]);
+      u.old_lo = half(o.lo[cur]);
+    }
+    u.ld_old = o.lp; u.s_old = xs;
+    u.m_store = (int)o.lp; u.n_store = (int)o.sp;
+    u.last = last;
+    const double to = last ? (double)p->scale : (double)o.steps.sx[t + 1];
+    u.f_old = (float)(to * (1.0 - fold) * p->a / sx);
+    u.f_acc = (float)(to / ((double)sp * sx));
+    if (last) {
+      u.out = dev_O;
+      u.ldo = p->ld_o; u.so = p->batch > 1 ? p->stride_o : 0;
+      u.out_dtype = p->out_dtype;
+      u.transpose_out = o.tall;
+    } else {
+      u.out = half(o.x[cur ^ 1]);
+      u.ldo = o.lp; u.so = xs;
+      u.out_lo = t + 2 < p->steps ? half(o.lo[cur ^ 1]) : nullptr;
+    }
+    e = launch_tiles(KIND_F16, EPI_UPDATE, u, o.update, st);
+  }
+  return e;
 }
 
 }  // namespace
@@ -293,7 +392,6 @@ int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_
   if (rc) return rc;
   const hipStream_t st = (hipStream_t)stream;
   char* ws = static_cast<char*>(dev_workspace);
-  auto half = [&](size_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
 
   OrthPrepArgs prep{};
   prep.p = *p;
@@ -301,80 +399,15 @@ int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_
   prep.M = dev_M;
   prep.parts = reinterpret_cast<double*>(ws + o.parts);
   prep.nparts = o.nparts;
-  prep.s = o.s; prep.l = o.l; prep.lp = o.lp; prep.tall = o.tall;
+  prep.s = o.s; prep.l = o.l; prep.sp = o.sp; prep.lp = o.lp; prep.tall = o.tall;
   prep.x_scale = o.steps.sx[0];
   if (orth_small_ok(o.s, o.l)) return hip_rc(launch_orth_small(prep, dev_O, o.steps, st));
   hipError_t e = launch_orth_norm(prep, st);
   if (e != hipSuccess) return hip_rc(e);
   if (p->steps == 0) return hip_rc(launch_orth_store(prep, dev_O, st));
-  prep.hi = half(o.x[0]);
-  prep.lo = half(o.lo[0]);
-  e = launch_orth_start(prep, st);
-
-  const int64_t xs = (int64_t)o.s * o.lp, qs = (int64_t)o.s * o.sp;     // elements of X, of S and P
-  for (int t = 0; t < p->steps && e == hipSuccess; ++t) {
-    const int cur = t & 1;
-    const bool last = t + 1 == p->steps;
-    const float sx = o.steps.sx[t], ss = o.steps.ss[t], sp = o.steps.sp[t], fold = o.steps.fold[t];
-    TileArgs g{};
-    g.A = g.B = reinterpret_cast<const uint8_t*>(half(o.x[cur]));
-    g.lda = g.ldb = o.lp * 2;
-    g.sa = g.sb = xs * 2;
-    g.m_rows = g.n_rows = o.s;
-    g.stages = (int)(o.lp / 64);
-    g.batch = p->batch;
-    g.part = reinterpret_cast<float*>(ws + o.part);
-    g.symmetric = true;
-    g.out = half(o.gram_at);
-    g.ldo = o.sp; g.so = qs;
-    g.m_store = (int)o.sp; g.n_store = o.s;
-    g.f_acc = ss / (sx * sx);
-    e = launch_tiles(KIND_F16, EPI_GRAM, g, o.gram, st);
-    if (e != hipSuccess) break;
-    TileArgs q = g;
-    q.A = q.B = reinterpret_cast<const uint8_t*>(half(o.gram_at));
-    q.lda = q.ldb = o.sp * 2;
-    q.sa = q.sb = qs * 2;
-    q.stages = (int)(o.sp / 64);
-    q.out = half(o.poly_at);
-    q.old_hi = half(o.gram_at);
-    q.ld_old = o.sp; q.s_old = qs;
-    q.f_old = (float)((double)p->b * sp / ss);
-    q.f_acc = (float)((double)p->c * sp / ((double)ss * ss));
-    q.f_eye = fold * p->a * sp;
-    e = launch_tiles(KIND_F16, EPI_POLY, q, o.poly, st);
-    if (e != hipSuccess) break;
-    TileArgs u{};
-    u.A = reinterpret_cast<const uint8_t*>(half(o.x[cur]));
-    u.lda = o.lp * 2; u.sa = xs * 2;
-    u.a_cols = (int)o.lp; u.k_rows = o.s;
-    u.B = reinterpret_cast<const uint8_t*>(half(o.poly_at));
-    u.ldb = o.sp * 2; u.sb = qs * 2;
-    u.m_rows = o.l; u.n_rows = o.s;
-    u.stages = (int)(o.sp / 64);
-    u.batch = p->batch;
-    u.part = g.part;
-    if (fold < 1.f) {           // (in the last step all of a X is in P: it needs no second half of X)
-      u.old_hi = half(o.x[cur]);
-      u.old_lo = half(o.lo[cur]);
-    }
-    u.ld_old = o.lp; u.s_old = xs;
-    u.m_store = (int)o.lp; u.n_store = o.s;
-    u.last = last;
-    const double to = last ? (double)p->scale : (double)o.steps.sx[t + 1];
-    u.f_old = (float)(to * (1.0 - fold) * p->a / sx);
-    u.f_acc = (float)(to / ((double)sp * sx));
-    if (last) {
-      u.out = dev_O;
-      u.ldo = p->ld_o; u.so = p->batch > 1 ? p->stride_o : 0;
-      u.out_dtype = p->out_dtype;
-      u.transpose_out = o.tall;
-    } else {
-      u.out = half(o.x[cur ^ 1]);
-      u.ldo = o.lp; u.so = xs;
-      u.out_lo = t + 2 < p->steps ? half(o.lo[cur ^ 1]) : nullptr;
-    }
-    e = launch_tiles(KIND_F16, EPI_UPDATE, u, o.update, st);
+  for (int first = 0; first < p->batch && e == hipSuccess; first += o.chunk) {
+    const int items = p->batch - first < o.chunk ? p->batch - first : o.chunk;
+    e = orth_chunk(*p, o, prep, dev_O, ws, first, items, st);
   }
   return hip_rc(e);
 }

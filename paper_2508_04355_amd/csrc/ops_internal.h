@@ -58,10 +58,10 @@ struct TileArgs {
   int64_t sa, sb;                // bytes between batch items
   const uint8_t *scale_a, *scale_b;   // 4-bit operands: scale tiles
   int m_rows, n_rows;            // valid rows of A and of B
-  int a_cols, k_rows;            // A with its rows contiguous: rows it is stored with (a multiple of 64) and valid k, else unused
+  int a_cols, k_rows;            // A with its rows contiguous: rows it is stored with and k it is stored with (multiples of 64, zeros beyond the valid), else unused
   int stages;                    // k in stages of 128 bytes a row
   int batch;
-  int split;                     // workgroups per tile, one range of stages each
+  int split, whole;              // tiles from number `whole` on have `split` workgroups, one range of stages each
   float* part;                   // partial tiles of a split product
   bool symmetric;                // only tiles with tile_m >= tile_n are computed
   // epilogue
@@ -76,9 +76,13 @@ struct TileArgs {
   bool last, transpose_out;      // EPI_UPDATE: out is the caller's O (bf16 or fp32); element (i, j) at out[i * ldo + j]
 };
 enum TileKind { KIND_F16 = 0, KIND_MX4 = 1 };
-// tile edge (64 or 128) and split for a product, and the bytes of partial tiles it then needs
-struct TilePlan { int tile, split; size_t part_bytes; };
-TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, int stages, int batch, bool symmetric);
+// tile edge (64, 128 or 256), split and the first tile that is, whether only one triangle of a symmetric product is computed, and the bytes of partial
+// tiles.  big_ok: tiles of 256 can address the operands (tile256_ok)
+struct TilePlan { int tile, split, whole; bool symmetric; size_t part_bytes; };
+TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, int stages, int batch, bool symmetric, bool big_ok);
+// 32-bit offsets inside an operand: 256 rows of `row_bytes`; k_rows of them where its rows are contiguous
+inline bool tile256_ok(int64_t row_bytes, int64_t k_rows) { return 256 * row_bytes < 0x7fffffff && k_rows * row_bytes < 0x7fffffff; }
+hipError_t launch_tiles_256(TileKind kind, TileEpi epi, const TileArgs& a, hipStream_t st);     // tile256_kernels.hip
 hipError_t launch_tiles(TileKind kind, TileEpi epi, const TileArgs& a, const TilePlan& plan, hipStream_t st);
 
 // ---- the orthogonalised update -------------------------------------------------------------------------
@@ -93,8 +97,8 @@ struct OrthPrepArgs {
   float* M;                      // or null
   double* parts;                 // [batch][nparts]
   int nparts;
-  uint16_t *hi, *lo;             // X: [batch][s][lp], s = shorter side, lp = longer side padded to 64
-  int64_t lp;
+  uint16_t *hi, *lo;             // X: [batch][sp][lp], the shorter and the longer side padded to 64 with zeros
+  int64_t sp, lp;
   int s, l;
   bool tall;
   float x_scale;                 // X is stored times this

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void orth_start_kernel(OrthPrepArgs a, int col
   const int64_t r0 = (int64_t)(blockIdx.x / col_tiles) * 64;
   const int c0 = (blockIdx.x % col_tiles) * 64;
   const float* M = a.M ? a.M + (int64_t)b * a.p.stride_m : nullptr;
-  const int64_t base = (int64_t)b * a.s * a.lp;
+  const int64_t base = (int64_t)b * a.sp * a.lp;
   auto put = [&](int64_t at, const float (&x)[8]) {
     f16x8_t h, l;
 #pragma unroll
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256) void orth_start_kernel(OrthPrepArgs a, int col
 #pragma unroll
     for (int i = 0; i < 8; ++i) g[i] = c0 + c + i < a.p.cols && row < a.p.rows ? g[i] * f : 0.f;
     if (!TALL) {
-      if (row < a.s && c0 + c < a.lp) put(row * a.lp + c0 + c, g);
+      if (row < a.sp && c0 + c < a.lp) put(row * a.lp + c0 + c, g);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) tile[r * 65 + c + i] = g[i];
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256) void orth_start_kernel(OrthPrepArgs a, int col
       float x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = tile[(r + i) * 65 + c];
-      if (c0 + c < a.s && r0 + r < a.lp) put((int64_t)(c0 + c) * a.lp + r0 + r, x);
+      if (c0 + c < a.sp && r0 + r < a.lp) put((int64_t)(c0 + c) * a.lp + r0 + r, x);
     }
   }
 }
@@ -174,6 +174,7 @@ constexpr int SMALL_THREADS = 512;
 struct OrthSmallArgs {
   OrthPrepArgs prep;
   void* out;
+  bool vec_out;                  // rows of the output aligned to four elements
   OrthSteps steps;
 };
 
@@ -193,7 +194,7 @@ __device__ __forceinline__ void put4(char* m, int row, int col, const float (&x)
   *reinterpret_cast<f16x4_t*>(m + row * PITCH + (swizzle(row, col >> 3) << 4) + (col & 7) * 2) = h;
 }
 
-template <int SP, int LP, bool BF16G>
+template <int SP, int LP, bool BF16G, bool VEC>
 __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int UP = LP + 1;                       // fp32 U in LDS: [SP][UP], before anything else lies there
@@ -207,35 +208,49 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
   float* U = reinterpret_cast<float*>(smem);
   double* red = reinterpret_cast<double*>(smem + SP * UP * 4 / 8 * 8 + 8);
   // G and M once; U by (short side, long side), zeros around it
-  for (int q = tid; q < SP * UP; q += SMALL_THREADS) U[q] = 0.f;
+  static_assert(SP % 4 == 0, "U in whole vectors");
+  for (int q = tid; q < SP * UP / 4; q += SMALL_THREADS) reinterpret_cast<f32x4_t*>(smem)[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   __syncthreads();
   double sum = 0.0;
   {
-    const int n = p.rows * p.cols;
+    // pieces of eight columns, all of a thread's (at most four or eight) on their way together
+    constexpr int PIECES = SP * LP / 8 / SMALL_THREADS < 4 ? SP * LP / 8 / SMALL_THREADS : 4;
     float* M = o.M ? o.M + (int64_t)b * p.stride_m : nullptr;
-    for (int q0 = tid; q0 < n; q0 += 8 * SMALL_THREADS) {
-      float x[8], m[8];
+    const int per_row = (p.cols + 7) / 8, n = p.rows * per_row;
+    for (int q0 = tid; q0 < n; q0 += PIECES * SMALL_THREADS) {
+      float x[PIECES][8], m[PIECES][8];
+      int row[PIECES], c[PIECES];
 #pragma unroll
-      for (int h = 0; h < 8; ++h) {
-        const int q = q0 + h * SMALL_THREADS, row = q / p.cols, c = q - row * p.cols;
-        x[h] = m[h] = 0.f;
-        if (q < n) {
-          const int64_t at = (int64_t)b * p.stride_g + row * p.ld_g + c;
-          x[h] = BF16G ? bf16_of(static_cast<const uint16_t*>(o.G)[at]) : static_cast<const float*>(o.G)[at];
-          if (M) m[h] = M[row * p.ld_m + c];
-        }
+      for (int h = 0; h < PIECES; ++h) {
+        const int q = q0 + h * SMALL_THREADS;
+        row[h] = q / per_row;
+        c[h] = (q - row[h] * per_row) * 8;
+        load_g<BF16G, VEC>(o, b, row[h], c[h], q < n, x[h]);
+        if (M) load8<true, VEC>(M, row[h] * p.ld_m + c[h], c[h], p.cols, q < n, m[h]);
       }
 #pragma unroll
-      for (int h = 0; h < 8; ++h) {
-        const int q = q0 + h * SMALL_THREADS, row = q / p.cols, c = q - row * p.cols;
-        if (q >= n) break;
+      for (int h = 0; h < PIECES; ++h) {
+        if (q0 + h * SMALL_THREADS >= n) break;
         if (M) {
-          m[h] = fmaf(p.mu, m[h], x[h]);
-          M[row * p.ld_m + c] = m[h];
-          x[h] = update_of(o, x[h], m[h]);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            m[h][i] = fmaf(p.mu, m[h][i], x[h][i]);
+            x[h][i] = update_of(o, x[h][i], m[h][i]);
+          }
+          float* to = M + row[h] * p.ld_m + c[h];
+          if (VEC && c[h] + 8 <= p.cols) {
+            reinterpret_cast<f32x4_t*>(to)[0] = f32x4_t{m[h][0], m[h][1], m[h][2], m[h][3]};
+            reinterpret_cast<f32x4_t*>(to)[1] = f32x4_t{m[h][4], m[h][5], m[h][6], m[h][7]};
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (c[h] + i < p.cols) to[i] = m[h][i];
+          }
         }
-        sum = fma((double)x[h], (double)x[h], sum);
-        U[(o.tall ? c : row) * UP + (o.tall ? row : c)] = x[h];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          sum = fma((double)x[h][i], (double)x[h][i], sum);
+          if (c[h] + i < p.cols) U[o.tall ? (c[h] + i) * UP + row[h] : row[h] * UP + c[h] + i] = x[h][i];
+        }
       }
     }
   }
@@ -257,7 +272,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
   __syncthreads();
   char* X = smem;
   char* S = smem + SP * XPITCH;
-  const int ksteps_l = (o.l + 31) / 32, ksteps_s = (o.s + 31) / 32;
+  constexpr int KL = LP / 32, KS = SP / 32;        // (zeros beyond the matrix)
   for (int t = 0; t < p.steps; ++t) {
     const float sx = a.steps.sx[t], ss = a.steps.ss[t], sp = a.steps.sp[t], fold = a.steps.fold[t];
 #pragma unroll
@@ -271,7 +286,8 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
     for (int i = 0; i < GI; ++i)
 #pragma unroll
       for (int j = 0; j < FJ; ++j) gram[i][j] = poly[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < ksteps_l; ++k) {
+#pragma unroll
+    for (int k = 0; k < KL; ++k) {
       f16x8_t fa[GI], fb[FJ];
 #pragma unroll
       for (int i = 0; i < GI; ++i) fa[i] = row_fragment<XPITCH>(X, (GI * wi + i) * 16 + l16, k * 4 + g);
@@ -296,7 +312,8 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
         put4<SPITCH>(S, (FJ * wj + j) * 16 + l16, (GI * wi + i) * 16 + 4 * g, y);
       }
     __syncthreads();
-    for (int k = 0; k < ksteps_s; ++k) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
       f16x8_t fa[GI], fb[FJ];
 #pragma unroll
       for (int i = 0; i < GI; ++i) fa[i] = row_fragment<SPITCH>(S, (GI * wi + i) * 16 + l16, k * 4 + g);
@@ -329,7 +346,8 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
     for (int i = 0; i < FI; ++i)
 #pragma unroll
       for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < ksteps_s; ++k) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
       f16x8_t fb[FJ];
 #pragma unroll
       for (int j = 0; j < FJ; ++j) fb[j] = row_fragment<SPITCH>(S, (FJ * wj + j) * 16 + l16, k * 4 + g);
@@ -356,30 +374,26 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
 #pragma unroll
   for (int i = 0; i < FI; ++i)
 #pragma unroll
-    for (int j = 0; j < FJ; ++j)
+    for (int j = 0; j < FJ; ++j) {
+      const int is = (FJ * wj + j) * 16 + l16, il = (FI * wi + i) * 16 + 4 * g;
+      if (is >= o.s) continue;
+      const int64_t at = (int64_t)b * p.stride_o + (o.tall ? il * p.ld_o + is : is * p.ld_o + il);
+      if (a.vec_out && !o.tall && il + 4 <= o.l) {
+        const float y0 = x[i][j][0] * last_f, y1 = x[i][j][1] * last_f, y2 = x[i][j][2] * last_f, y3 = x[i][j][3] * last_f;
+        if (p.out_dtype == GECC_F32) *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + at) = f32x4_t{y0, y1, y2, y3};
+        else *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(a.out) + at) =
+                 u32x2_t{(unsigned)to_bf16(y0) | ((unsigned)to_bf16(y1) << 16), (unsigned)to_bf16(y2) | ((unsigned)to_bf16(y3) << 16)};
+        continue;
+      }
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int is = (FJ * wj + j) * 16 + l16, il = (FI * wi + i) * 16 + 4 * g + v;
-        if (is >= o.s || il >= o.l) continue;
-        const int64_t at = (int64_t)b * p.stride_o + (o.tall ? il * p.ld_o + is : is * p.ld_o + il);
+        if (il + v >= o.l) continue;
+        const int64_t to = at + v * (o.tall ? p.ld_o : 1);
         const float y = x[i][j][v] * last_f;
-        if (p.out_dtype == GECC_F32) static_cast<float*>(a.out)[at] = y;
-        else static_cast<uint16_t*>(a.out)[at] = to_bf16(y);
+        if (p.out_dtype == GECC_F32) static_cast<float*>(a.out)[to] = y;
+        else static_cast<uint16_t*>(a.out)[to] = to_bf16(y);
       }
-}
-
-template <int SP, int LP>
-hipError_t small(const OrthSmallArgs& a, hipStream_t st) {
-  constexpr int u_bytes = SP * (LP + 1) * 4 / 8 * 8 + 8 + 64, x_bytes = SP * (LP * 2 < 256 ? 256 : LP * 2) + SP * 256;
-  constexpr int lds = u_bytes > x_bytes ? u_bytes : x_bytes;
-  auto kern = a.prep.p.dtype == GECC_BF16 ? orth_small_kernel<SP, LP, true> : orth_small_kernel<SP, LP, false>;
-  if (lds > 65536) {
-    static LdsLimit limit[2];
-    const hipError_t e = limit[a.prep.p.dtype == GECC_BF16].raise(reinterpret_cast<const void*>(kern), lds);
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(kern, dim3(a.prep.p.batch), dim3(SMALL_THREADS), lds, st, a);
-  return hipGetLastError();
+    }
 }
 
 bool vectors_ok(const OrthPrepArgs& a) {
@@ -387,6 +401,22 @@ bool vectors_ok(const OrthPrepArgs& a) {
   if (reinterpret_cast<uintptr_t>(a.G) % 16 || a.p.ld_g * es % 16 || (a.p.batch > 1 && a.p.stride_g * es % 16)) return false;
   if (!a.M) return true;
   return reinterpret_cast<uintptr_t>(a.M) % 16 == 0 && a.p.ld_m % 4 == 0 && (a.p.batch == 1 || a.p.stride_m % 4 == 0);
+}
+
+template <int SP, int LP>
+hipError_t small(const OrthSmallArgs& a, hipStream_t st) {
+  constexpr int u_bytes = SP * (LP + 1) * 4 / 8 * 8 + 8 + 64, x_bytes = SP * (LP * 2 < 256 ? 256 : LP * 2) + SP * 256;
+  constexpr int lds = u_bytes > x_bytes ? u_bytes : x_bytes;
+  const bool bf16 = a.prep.p.dtype == GECC_BF16, vec = vectors_ok(a.prep);
+  auto kern = bf16 ? (vec ? orth_small_kernel<SP, LP, true, true> : orth_small_kernel<SP, LP, true, false>)
+                   : (vec ? orth_small_kernel<SP, LP, false, true> : orth_small_kernel<SP, LP, false, false>);
+  if (lds > 65536) {
+    static LdsLimit limit[4];
+    const hipError_t e = limit[2 * bf16 + vec].raise(reinterpret_cast<const void*>(kern), lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kern, dim3(a.prep.p.batch), dim3(SMALL_THREADS), lds, st, a);
+  return hipGetLastError();
 }
 
 template <bool BF16G, bool VEC>
@@ -424,7 +454,9 @@ bool orth_small_ok(int s, int l) { return s <= 128 && l <= 256; }
 
 hipError_t launch_orth_small(const OrthPrepArgs& prep, void* out, const OrthSteps& steps, hipStream_t st) {
   if (!orth_small_ok(prep.s, prep.l)) return hipErrorInvalidValue;
-  const OrthSmallArgs a = {prep, out, steps};
+  const int es = prep.p.out_dtype == GECC_F32 ? 4 : 2;
+  const bool vec_out = reinterpret_cast<uintptr_t>(out) % (4 * es) == 0 && prep.p.ld_o % 4 == 0 && (prep.p.batch == 1 || prep.p.stride_o % 4 == 0);
+  const OrthSmallArgs a = {prep, out, vec_out, steps};
   if (prep.s <= 64) return prep.l <= 128 ? small<64, 128>(a, st) : small<64, 256>(a, st);
   return prep.l <= 128 ? small<128, 128>(a, st) : small<128, 256>(a, st);
 }

@@ -1,0 +1,94 @@
+// Products on fp16 and on microscaled 4-bit operands in tiles of 256 x 256, for the operators of gecc_ops.h: the main loop
+// of the bf16 product (tile256_device.h), whose operands' bytes are the same, and the operators' epilogues.
+#include "ops_internal.h"
+#include "tile256_device.h"
+#include "tile_epilogue.h"
+#include "lds_limit.h"
+
+namespace gecc {
+namespace {
+
+// A: k-contiguous or (KCA false) with its rows contiguous; B: k-contiguous.  The grid is tiles, those from number `whole` on
+// `split` times, x batch.
+template <int KIND, bool KCA, int EPI>
+__global__ __launch_bounds__(THREADS, 1) void tile256_kernel(TileArgs a, bool vec_out) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wr = wave >> 1, wc = wave & 1;
+  const int b = blockIdx.y;
+  int tile = blockIdx.x, range = 0;
+  const bool shared = tile >= a.whole;
+  if (shared) {
+    const unsigned y = tile - a.whole;
+    tile = a.whole + y / (unsigned)a.split;
+    range = y % (unsigned)a.split;
+  }
+  int tm, tn;
+  if (a.symmetric) triangle(tile, tm, tn);
+  else tile_of(tile, (a.m_rows + BM - 1) / BM, (a.n_rows + BN - 1) / BN, 0, 0, tm, tn);
+  const int r0 = tm * BM, c0 = tn * BN;
+  // stages of 128 bytes of k (a pair of k-tiles), shared out in twos: four k-tiles have their scales in one word
+  const int twos = (a.stages + 1) / 2;
+  int first = 0, last = a.stages;
+  if (shared) {
+    first = (int)((unsigned)twos * range / (unsigned)a.split) * 2;
+    last = min((int)((unsigned)twos * (range + 1) / (unsigned)a.split) * 2, a.stages);
+  }
+  const int NP = last - first, KT = 2 * NP;
+
+  Operand<KCA> oa;
+  Operand<true> ob;
+  const int64_t lda = a.lda / 2, ldb = a.ldb / 2;         // in units of 16 bits, as the loop counts
+  const uint16_t* A = reinterpret_cast<const uint16_t*>(a.A + b * a.sa) + (KCA ? (int64_t)first * 64 : (int64_t)first * 64 * lda);
+  const uint16_t* B = reinterpret_cast<const uint16_t*>(a.B + b * a.sb) + (int64_t)first * 64;
+  oa.init(A, lda, r0, KCA ? a.m_rows : a.a_cols, KCA ? 0 : a.k_rows - first * 64, wr * 128);
+  ob.init(B, ldb, c0, a.n_rows, 0, wc * 128);
+  Scales256 sc{};
+  if (KIND == KIND_MX4) sc.init(a.scale_a, a.scale_b, r0, c0, a.m_rows, a.n_rows, twos, first / 2);
+
+  f32x4_t acc[8][8];
+  // the k order's start, as in the bf16 product; in twos of pairs for the scales
+  int p0 = ((tm & 7) * SKEW_M + (tn & 3) * SKEW_N) % NP;
+  if (KIND == KIND_MX4) p0 = NP % 2 ? 0 : (2 * ((tm & 7) * SKEW_M + (tn & 3) * SKEW_N)) % NP;
+  multiply_256<KIND == KIND_MX4 ? T256_MX4 : T256_F16, KCA, true, true>(acc, oa, ob, sc, smem, KT, __builtin_amdgcn_readfirstlane(p0));
+
+  if (shared) {               // in the order of the registers, as tile_finish_kernel takes them
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + ((int64_t)b * (gridDim.x - a.whole) + (blockIdx.x - a.whole)) * (BM * BN / 4) + wave * 4096 + lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[(i * 8 + j) * 64] = acc[i][j];
+    return;
+  }
+  store_tile<EPI, 8, 8>(a, b, acc, reinterpret_cast<float*>(smem) + wave * store_floats<8>(), r0 + wr * 128, c0 + wc * 128, r0 + BM, c0 + BN,
+                         a.symmetric && tm != tn, vec_out);
+}
+
+template <int KIND, bool KCA, int EPI>
+hipError_t launch(const TileArgs& a, hipStream_t st) {
+  const int64_t tm = (a.m_rows + BM - 1) / BM, tn = (a.n_rows + BN - 1) / BN;
+  const int64_t tiles = a.symmetric ? tm * (tm + 1) / 2 : tm * tn;
+  const int64_t groups = a.whole + (tiles - a.whole) * a.split;
+  if (groups > 0x7fffffff || a.batch > 65535 || a.whole > tiles || a.split < 1 || a.split > (a.stages + 1) / 2) return hipErrorInvalidValue;
+  constexpr int lds = KIND == KIND_MX4 ? SMEM_MX_BYTES : SMEM_BYTES;
+  auto kern = tile256_kernel<KIND, KCA, EPI>;
+  static LdsLimit limit;
+  const hipError_t e = limit.raise(reinterpret_cast<const void*>(kern), lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)groups, a.batch), dim3(THREADS), lds, st, a, vectors_out(a, 8));
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_tiles_256(TileKind kind, TileEpi epi, const TileArgs& a, hipStream_t st) {
+  if (kind == KIND_MX4) return launch<KIND_MX4, true, EPI_OUT>(a, st);
+  switch (epi) {
+    case EPI_GRAM: return launch<KIND_F16, true, EPI_GRAM>(a, st);
+    case EPI_POLY: return launch<KIND_F16, true, EPI_POLY>(a, st);
+    case EPI_UPDATE: return launch<KIND_F16, false, EPI_UPDATE>(a, st);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace gecc

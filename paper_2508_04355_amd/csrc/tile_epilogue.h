@@ -1,0 +1,232 @@
+// What becomes of a tile of D (see ops_internal.h), N = 4 or 8 values of consecutive i a call.
+#pragma once
+#include <type_traits>
+#include "ops_internal.h"
+#include "ops_device.h"
+
+namespace gecc {
+namespace {
+
+template <int N>
+struct Vectors {
+  typedef __attribute__((ext_vector_type(N))) _Float16 half_t;
+  typedef __attribute__((ext_vector_type(N / 2))) unsigned word_t;     // N bf16
+};
+
+template <int N>
+__device__ __forceinline__ typename Vectors<N>::word_t bf16_words(const float (&x)[N]) {
+  typename Vectors<N>::word_t w;
+#pragma unroll
+  for (int v = 0; v < N / 2; ++v) w[v] = (unsigned)to_bf16(x[2 * v]) | ((unsigned)to_bf16(x[2 * v + 1]) << 16);
+  return w;
+}
+
+// ---- N elements (i .. i + N - 1, j) of D; i is a multiple of N -------------------------------------------------------
+// what an element's old value is made from; OLD: there is one (else nothing is read)
+template <int N>
+struct Old { typename Vectors<N>::half_t hi, lo; };
+template <int EPI, int N, bool OLD>
+__device__ __forceinline__ void load_old(const TileArgs& a, int b, int i, int j, Old<N>& o) {
+  if (!OLD) return;
+  typedef typename Vectors<N>::half_t half_t;
+  const int64_t at = b * a.s_old + (int64_t)j * a.ld_old + i;
+  o.hi = *reinterpret_cast<const half_t*>(a.old_hi + at);
+  if (EPI == EPI_UPDATE) o.lo = *reinterpret_cast<const half_t*>(a.old_lo + at);
+}
+// the values to store, from the accumulators (not EPI_OUT)
+template <int EPI, int N, bool OLD>
+__device__ __forceinline__ void finished(const TileArgs& a, int i, int j, const float (&acc)[N], const Old<N>& o, float (&x)[N]) {
+#pragma unroll
+  for (int v = 0; v < N; ++v) {
+    float old = 0.f;
+    if (OLD) old = EPI == EPI_UPDATE ? (float)o.hi[v] + (float)o.lo[v] : (float)o.hi[v];
+    x[v] = fmaf(a.f_old, old, a.f_acc * acc[v]);
+    if (EPI == EPI_POLY && i + v == j) x[v] += a.f_eye;
+  }
+}
+template <int N>
+__device__ __forceinline__ void put_f32(float* o, const float (&x)[N]) {
+#pragma unroll
+  for (int v = 0; v < N; v += 4) __builtin_nontemporal_store(f32x4_t{x[v], x[v + 1], x[v + 2], x[v + 3]}, reinterpret_cast<f32x4_t*>(o + v));
+}
+template <int N>
+__device__ __forceinline__ void put_bf16(uint16_t* o, const float (&x)[N]) {
+  __builtin_nontemporal_store(bf16_words<N>(x), reinterpret_cast<typename Vectors<N>::word_t*>(o));
+}
+// fp16, and what its rounding leaves where LO
+template <int N, bool LO>
+__device__ __forceinline__ void put_f16(const TileArgs& a, int64_t at, const float (&x)[N]) {
+  typename Vectors<N>::half_t h, l;
+#pragma unroll
+  for (int v = 0; v < N; ++v) h[v] = (_Float16)x[v];
+  *reinterpret_cast<typename Vectors<N>::half_t*>(static_cast<uint16_t*>(a.out) + at) = h;
+  if (LO) {
+#pragma unroll
+    for (int v = 0; v < N; ++v) l[v] = (_Float16)(x[v] - (float)h[v]);
+    *reinterpret_cast<typename Vectors<N>::half_t*>(a.out_lo + at) = l;
+  }
+}
+
+// Any tile.  vec_out: the caller's rows are aligned to N elements
+template <int EPI, int N>
+__device__ __forceinline__ void store_elements(const TileArgs& a, int b, int i, int j, bool mirror, const float (&acc)[N], bool vec_out) {
+  const int64_t at = b * a.so + (int64_t)j * a.ldo + i;
+  if (EPI == EPI_OUT) {
+    if (j >= a.n_rows || i >= a.m_rows) return;
+    const bool whole = vec_out && i + N <= a.m_rows;
+    if (a.out_dtype == GECC_F32) {
+      float* o = static_cast<float*>(a.out) + at;
+      if (whole) put_f32<N>(o, acc);
+      else {
+#pragma unroll
+        for (int v = 0; v < N; ++v) if (i + v < a.m_rows) o[v] = acc[v];
+      }
+    } else {
+      uint16_t* o = static_cast<uint16_t*>(a.out) + at;
+      if (whole) put_bf16<N>(o, acc);
+      else {
+#pragma unroll
+        for (int v = 0; v < N; ++v) if (i + v < a.m_rows) o[v] = to_bf16(acc[v]);
+      }
+    }
+    return;
+  }
+  // (the internal matrices: i is stored in whole groups up to m_store, a multiple of 64)
+  if (j >= a.n_store || i >= a.m_store) return;
+  float x[N];
+  Old<N> o;
+  if (EPI == EPI_POLY || (EPI == EPI_UPDATE && a.old_hi)) {
+    load_old<EPI, N, true>(a, b, i, j, o);
+    finished<EPI, N, true>(a, i, j, acc, o, x);
+  } else {
+    finished<EPI, N, false>(a, i, j, acc, o, x);
+  }
+  if (EPI == EPI_UPDATE && a.last) {
+    if (vec_out && !a.transpose_out && a.out_dtype == GECC_BF16 && i + N <= a.m_rows && j < a.n_rows) {
+      put_bf16<N>(static_cast<uint16_t*>(a.out) + at, x);
+      return;
+    }
+#pragma unroll
+    for (int v = 0; v < N; ++v) {
+      if (i + v >= a.m_rows || j >= a.n_rows) continue;
+      const int64_t to = a.transpose_out ? b * a.so + (int64_t)(i + v) * a.ldo + j : at + v;
+      if (a.out_dtype == GECC_F32) static_cast<float*>(a.out)[to] = x[v];
+      else static_cast<uint16_t*>(a.out)[to] = to_bf16(x[v]);
+    }
+    return;
+  }
+  if (EPI == EPI_UPDATE && a.out_lo) put_f16<N, true>(a, at, x);
+  else put_f16<N, false>(a, at, x);
+  if (EPI != EPI_UPDATE && mirror && j < a.m_store) {
+    uint16_t* out = static_cast<uint16_t*>(a.out) + b * a.so;
+#pragma unroll
+    for (int v = 0; v < N; ++v) {
+      const _Float16 y = (_Float16)x[v];      // (not an element of a vector: this compiler's bit cast of one takes the first)
+      if (i + v < a.n_store) out[(int64_t)(i + v) * a.ldo + j] = __builtin_bit_cast(uint16_t, y);
+    }
+  }
+}
+
+// A tile that lies inside, with everything that could be asked per element known beforehand: no branches between the
+// stores, so that their loads, conversions and stores overlap (16384 x 4096 x 14336 on 4 bits: the epilogue of a 256 x 256
+// tile took 14 600 cycles with the tests of store_elements in it)
+enum { IN_F32 = 0, IN_BF16 = 1, IN_HALF = 2, IN_HALVES = 3 };
+template <int EPI, int N, int HOW, bool OLD>
+__device__ __forceinline__ void store_inside(const TileArgs& a, int b, int i, int j, const float (&acc)[N], const Old<N>& o) {
+  const int64_t at = b * a.so + (int64_t)j * a.ldo + i;
+  float x[N];
+  if (EPI == EPI_OUT) {
+#pragma unroll
+    for (int v = 0; v < N; ++v) x[v] = acc[v];
+  } else {
+    finished<EPI, N, OLD>(a, i, j, acc, o, x);
+  }
+  if (HOW == IN_F32) put_f32<N>(static_cast<float*>(a.out) + at, x);
+  else if (HOW == IN_BF16) put_bf16<N>(static_cast<uint16_t*>(a.out) + at, x);
+  else put_f16<N, HOW == IN_HALVES>(a, at, x);
+}
+
+// A wavefront's FI x FJ blocks of accumulators, from element (i0, j0) on.  A lane holds four consecutive i of sixteen j: a
+// store from there would write 32-byte pieces.  Through LDS (the wavefront's own 2 x 16 rows of 16 FI + 4 floats at `st`; the
+// 4 keep 16 rows off each other's banks) sixteen j at a time become rows of 16 FI consecutive i, eight a lane.
+template <int FI>
+constexpr int store_floats() { return 2 * 16 * (16 * FI + 4); }
+// each(i, j, x, old): eight elements from (i, j) on; load(i, j, old) is called AHEAD groups of sixteen j earlier
+template <int FI, int FJ, class L, class F>
+__device__ __forceinline__ void by_rows(const f32x4_t (&acc)[FI][FJ], float* st, int i0, int j0, L&& load, F&& each) {
+  constexpr int PITCH = 16 * FI + 4, LANES = 2 * FI, ROWS = 64 / LANES, Q = 16 / ROWS;
+  constexpr int AHEAD = 2;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const int i = i0 + (lane % LANES) * 8, jl = j0 + lane / LANES;
+  Old<8> old[AHEAD][Q];
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+    for (int q = 0; q < Q; ++q) load(i, jl + 16 * j + q * ROWS, old[j][q]);
+#pragma unroll
+  for (int j = 0; j < FJ; ++j) {
+    float* buf = st + (j & 1) * 16 * PITCH;
+#pragma unroll
+    for (int f = 0; f < FI; ++f) *reinterpret_cast<f32x4_t*>(buf + l16 * PITCH + 16 * f + 4 * g) = acc[f][j];
+    __builtin_amdgcn_wave_barrier();            // (the LDS takes a wavefront's instructions in order)
+    float x[Q][8];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const float* p = buf + (q * ROWS + lane / LANES) * PITCH + (lane % LANES) * 8;
+      const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(p), hi = *reinterpret_cast<const f32x4_t*>(p + 4);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) { x[q][v] = lo[v]; x[q][4 + v] = hi[v]; }
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < Q; ++q) each(i, jl + 16 * j + q * ROWS, x[q], old[j % AHEAD][q]);
+    if (j + AHEAD < FJ) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) load(i, jl + 16 * (j + AHEAD) + q * ROWS, old[j % AHEAD][q]);
+    }
+  }
+}
+// i_end, j_end: the ends of the workgroup's whole tile
+template <int EPI, int FI, int FJ>
+__device__ __forceinline__ void store_tile(const TileArgs& a, int b, const f32x4_t (&acc)[FI][FJ], float* st, int i0, int j0, int i_end, int j_end,
+                                           bool mirror, bool vec_out) {
+  auto inside = [&](auto how_c, auto old_c) {
+    constexpr bool OLD = decltype(old_c)::value;
+    by_rows<FI, FJ>(acc, st, i0, j0, [&](int i, int j, Old<8>& o) { load_old<EPI, 8, OLD>(a, b, i, j, o); },
+                    [&](int i, int j, const float (&x)[8], const Old<8>& o) { store_inside<EPI, 8, decltype(how_c)::value, OLD>(a, b, i, j, x, o); });
+  };
+  using std::integral_constant;
+  if (EPI == EPI_OUT) {
+    if (vec_out && i_end <= a.m_rows && j_end <= a.n_rows) {
+      if (a.out_dtype == GECC_F32) inside(integral_constant<int, IN_F32>{}, std::false_type{});
+      else inside(integral_constant<int, IN_BF16>{}, std::false_type{});
+      return;
+    }
+  } else if (EPI == EPI_UPDATE) {
+    if (a.last) {
+      if (vec_out && !a.old_hi && !a.transpose_out && a.out_dtype == GECC_BF16 && i_end <= a.m_rows && j_end <= a.n_rows) {
+        inside(integral_constant<int, IN_BF16>{}, std::false_type{});
+        return;
+      }
+    } else if (a.old_hi && i_end <= a.m_store && j_end <= a.n_store) {
+      if (a.out_lo) inside(integral_constant<int, IN_HALVES>{}, std::true_type{});
+      else inside(integral_constant<int, IN_HALF>{}, std::true_type{});
+      return;
+    }
+  } else if (!mirror && i_end <= a.m_store && j_end <= a.n_store) {
+    inside(integral_constant<int, IN_HALF>{}, integral_constant<bool, EPI == EPI_POLY>{});
+    return;
+  }
+  by_rows<FI, FJ>(acc, st, i0, j0, [](int, int, Old<8>&) {},
+                  [&](int i, int j, const float (&x)[8], const Old<8>&) { store_elements<EPI, 8>(a, b, i, j, mirror, x, vec_out); });
+}
+
+// whether the caller's output takes vectors of n elements
+inline bool vectors_out(const TileArgs& a, int n) {
+  const int es = a.out_dtype == GECC_F32 ? 4 : 2;
+  const int64_t align = n * es > 16 ? 16 : n * es, per = align / es;
+  return reinterpret_cast<uintptr_t>(a.out) % align == 0 && a.ldo % per == 0 && a.so % per == 0;
+}
+
+}  // namespace
+}  // namespace gecc

@@ -17,92 +17,19 @@
 #include "dma_device.h"
 #include "ops_device.h"
 #include "lds_limit.h"
+#include "tile_epilogue.h"
+#include "tile_order.h"
 
 namespace gecc {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
-typedef __attribute__((ext_vector_type(4))) _Float16 f16x4_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((ext_vector_type(8))) short s16x8_t;
 typedef __attribute__((ext_vector_type(8))) int i32x8_t;
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
 constexpr int THREADS = 256;
-
-// ---- what becomes of a tile: element (i, j) of D, four values i .. i + 3 a call -------------------------------------
-template <int EPI>
-__device__ __forceinline__ void store4(const TileArgs& a, int b, int i, int j, bool mirror, const f32x4_t& acc, bool vec_out) {
-  if (EPI == EPI_OUT) {
-    if (j >= a.n_rows || i >= a.m_rows) return;
-    if (a.out_dtype == GECC_F32) {
-      float* o = static_cast<float*>(a.out) + b * a.so + (int64_t)j * a.ldo + i;
-      if (vec_out && i + 4 <= a.m_rows) *reinterpret_cast<f32x4_t*>(o) = acc;
-      else
-        for (int v = 0; v < 4; ++v) if (i + v < a.m_rows) o[v] = acc[v];
-    } else {
-      uint16_t* o = static_cast<uint16_t*>(a.out) + b * a.so + (int64_t)j * a.ldo + i;
-      if (vec_out && i + 4 <= a.m_rows)
-        *reinterpret_cast<u32x2_t*>(o) = u32x2_t{(unsigned)to_bf16(acc[0]) | ((unsigned)to_bf16(acc[1]) << 16),
-                                                 (unsigned)to_bf16(acc[2]) | ((unsigned)to_bf16(acc[3]) << 16)};
-      else
-        for (int v = 0; v < 4; ++v) if (i + v < a.m_rows) o[v] = to_bf16(acc[v]);
-    }
-    return;
-  }
-  // (the internal matrices: i is stored in groups of four up to m_store, a multiple of 64)
-  if (j >= a.n_store || i >= a.m_store) return;
-  float x[4];
-  if (EPI == EPI_GRAM) {
-#pragma unroll
-    for (int v = 0; v < 4; ++v) x[v] = a.f_acc * acc[v];
-  } else {
-    const int64_t at = b * a.s_old + (int64_t)j * a.ld_old + i;
-    float old[4] = {0.f, 0.f, 0.f, 0.f};
-    if (EPI == EPI_POLY || a.old_hi) {
-      const f16x4_t hi = *reinterpret_cast<const f16x4_t*>(a.old_hi + at);
-      f16x4_t lo = {0, 0, 0, 0};
-      if (EPI == EPI_UPDATE) lo = *reinterpret_cast<const f16x4_t*>(a.old_lo + at);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) old[v] = (float)hi[v] + (float)lo[v];
-    }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      x[v] = fmaf(a.f_old, old[v], a.f_acc * acc[v]);
-      if (EPI == EPI_POLY && i + v == j) x[v] += a.f_eye;
-    }
-  }
-  if (EPI == EPI_UPDATE && a.last) {
-    // (no loops over the four with a run-time end: the caller's rows and columns end anywhere)
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      if (i + v >= a.m_rows || j >= a.n_rows) continue;
-      const int64_t at = b * a.so + (a.transpose_out ? (int64_t)(i + v) * a.ldo + j : (int64_t)j * a.ldo + i + v);
-      if (a.out_dtype == GECC_F32) static_cast<float*>(a.out)[at] = x[v];
-      else static_cast<uint16_t*>(a.out)[at] = to_bf16(x[v]);
-    }
-    return;
-  }
-  uint16_t* out = static_cast<uint16_t*>(a.out) + b * a.so;
-  f16x4_t h;
-#pragma unroll
-  for (int v = 0; v < 4; ++v) h[v] = (_Float16)x[v];
-  *reinterpret_cast<f16x4_t*>(out + (int64_t)j * a.ldo + i) = h;
-  if (EPI == EPI_UPDATE) {
-    if (a.out_lo) {
-      f16x4_t l;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) l[v] = (_Float16)(x[v] - (float)h[v]);
-      *reinterpret_cast<f16x4_t*>(a.out_lo + b * a.so + (int64_t)j * a.ldo + i) = l;
-    }
-  } else if (mirror && j < a.m_store) {
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const _Float16 y = (_Float16)x[v];      // (not an element of h: this compiler's bit cast of one takes the first)
-      if (i + v < a.n_store) out[(int64_t)(i + v) * a.ldo + j] = __builtin_bit_cast(uint16_t, y);
-    }
-  }
-}
 
 // ---- operands --------------------------------------------------------------------------------------------------------
 // KC: k-contiguous.  Otherwise (fp16): element (row, k) at P[k * ld + row].
@@ -170,14 +97,6 @@ struct TileOperand {
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 };
-
-// the index of a tile in the lower triangle: tm >= tn
-__device__ __forceinline__ void triangle(int t, int& tm, int& tn) {
-  tm = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-  while (tm * (tm + 1) / 2 > t) --tm;
-  while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-  tn = t - tm * (tm + 1) / 2;
-}
 
 template <int T>
 __device__ __forceinline__ void tile_at(const TileArgs& a, int t, int& tm, int& tn) {
@@ -304,42 +223,42 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
   }
 
   if (a.split > 1) {
-    // [batch][range][tile][fragment pair][lane] in the order of the registers; tile_finish_kernel adds the ranges up
-    const int64_t tiles = gridDim.x;
-    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + (((int64_t)b * a.split + blockIdx.y) * tiles + blockIdx.x) * (T * T / 4) + wave * (F * F * 64) + lane;
+    // [batch][tile][range][fragment pair][lane] in the order of the registers; tile_finish_kernel adds the ranges up
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + (((int64_t)b * gridDim.x + blockIdx.x) * a.split + blockIdx.y) * (T * T / 4) + wave * (F * F * 64) + lane;
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
       for (int j = 0; j < F; ++j) p[(i * F + j) * 64] = acc[i][j];
     return;
   }
-#pragma unroll
-  for (int i = 0; i < F; ++i)
-#pragma unroll
-    for (int j = 0; j < F; ++j)
-      store4<EPI>(a, b, r0 + wr * (T / 2) + i * 16 + 4 * g, c0 + wc * (T / 2) + j * 16 + l16, tm != tn, acc[i][j], vec_out);
+  __syncthreads();               // the stages are done with: their LDS holds rows of the result now
+  static_assert(4 * store_floats<F>() * 4 <= RING * SLOT, "room for the epilogue");
+  store_tile<EPI, F, F>(a, b, acc, reinterpret_cast<float*>(smem) + wave * store_floats<F>(), r0 + wr * (T / 2), c0 + wc * (T / 2), r0 + T, c0 + T,
+                         a.symmetric && tm != tn, vec_out);
 }
 
 // Adds the ranges of a split product up, in their order, and stores the result: a wavefront per fragment pair.
 template <int T, int EPI>
-__global__ __launch_bounds__(256) void tile_finish_kernel(TileArgs a, bool vec_out, int tiles) {
+__global__ __launch_bounds__(256) void tile_finish_kernel(TileArgs a, bool vec_out, int shared) {
   constexpr int F = T / 32;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
-  const int piece = blockIdx.x * 4 + (threadIdx.x >> 6);        // of tiles * 4 F F
+  const int piece = blockIdx.x * 4 + (threadIdx.x >> 6);        // of shared * 4 F F
   const int b = blockIdx.y;
-  const int t = piece / (4 * F * F), r = piece % (4 * F * F);
-  if (t >= tiles) return;
+  const int t = piece / (4 * F * F), r = piece % (4 * F * F);   // t: of the `shared` tiles from number a.whole on
+  if (t >= shared) return;
   int tm, tn;
-  tile_at<T>(a, t, tm, tn);
+  if (T == 256 && !a.symmetric) tile_of(a.whole + t, (a.m_rows + T - 1) / T, (a.n_rows + T - 1) / T, 0, 0, tm, tn);
+  else tile_at<T>(a, a.whole + t, tm, tn);
   const int wave = r / (F * F), i = r % (F * F) / F, j = r % F;
-  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(a.part) + ((int64_t)b * a.split * tiles + t) * (T * T / 4) + r * 64 + lane;
+  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(a.part) + ((int64_t)b * shared + t) * a.split * (T * T / 4) + r * 64 + lane;
   f32x4_t s = p[0];
   for (int q = 1; q < a.split; ++q) {
-    const f32x4_t x = p[(int64_t)q * tiles * (T * T / 4)];
+    const f32x4_t x = p[q * (T * T / 4)];
 #pragma unroll
     for (int v = 0; v < 4; ++v) s[v] += x[v];
   }
-  store4<EPI>(a, b, tm * T + (wave >> 1) * (T / 2) + i * 16 + 4 * g, tn * T + (wave & 1) * (T / 2) + j * 16 + l16, tm != tn, s, vec_out);
+  const float x[4] = {s[0], s[1], s[2], s[3]};
+  store_elements<EPI, 4>(a, b, tm * T + (wave >> 1) * (T / 2) + i * 16 + 4 * g, tn * T + (wave & 1) * (T / 2) + j * 16 + l16, a.symmetric && tm != tn, x, vec_out);
 }
 
 int64_t tiles_of(int64_t m_rows, int64_t n_rows, int T, bool symmetric) {
@@ -347,16 +266,19 @@ int64_t tiles_of(int64_t m_rows, int64_t n_rows, int T, bool symmetric) {
   return symmetric ? tm * (tm + 1) / 2 : tm * tn;
 }
 
+template <int T, int EPI>
+hipError_t launch_finish(const TileArgs& a, int64_t tiles, hipStream_t st) {
+  constexpr int F = T / 32;
+  const int64_t shared = tiles - a.whole;
+  hipLaunchKernelGGL((tile_finish_kernel<T, EPI>), dim3((unsigned)(shared * F * F), a.batch), dim3(256), 0, st, a, vectors_out(a, 4), (int)shared);
+  return hipGetLastError();
+}
+
 template <int KIND, bool KCA, int T, int RING, int EPI>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
   static_assert(RING == 2 || RING == 4, "the waits of tile_kernel");
   const int64_t tiles = tiles_of(a.m_rows, a.n_rows, T, a.symmetric);
   if (tiles > 0x7fffffff || a.batch > 65535) return hipErrorInvalidValue;
-  bool vec = false;
-  if (EPI == EPI_OUT) {
-    const int es = a.out_dtype == GECC_F32 ? 4 : 2;
-    vec = reinterpret_cast<uintptr_t>(a.out) % (4 * es) == 0 && a.ldo % 4 == 0 && a.so % 4 == 0;
-  }
   constexpr int lds = RING * 2 * T * 128 + (KIND == KIND_MX4 ? RING / 2 * 2 * T * 16 : 0);
   auto kern = tile_kernel<KIND, KCA, T, RING, EPI>;
   if (lds > 65536) {
@@ -364,27 +286,43 @@ hipError_t launch(const TileArgs& a, hipStream_t st) {
     const hipError_t e = limit.raise(reinterpret_cast<const void*>(kern), lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kern, dim3((unsigned)tiles, a.split, a.batch), dim3(THREADS), lds, st, a, vec);
+  hipLaunchKernelGGL(kern, dim3((unsigned)tiles, a.split, a.batch), dim3(THREADS), lds, st, a, vectors_out(a, 8));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.split == 1) return e;
-  constexpr int F = T / 32;
-  hipLaunchKernelGGL((tile_finish_kernel<T, EPI>), dim3((unsigned)(tiles * F * F), a.batch), dim3(256), 0, st, a, vec, (int)tiles);
-  return hipGetLastError();
+  return launch_finish<T, EPI>(a, tiles, st);
 }
 
 }  // namespace
 
-TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, int stages, int batch, bool symmetric) {
+TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, int stages, int batch, bool symmetric, bool big_ok) {
   TilePlan p;
-  // 128 x 128 tiles once they fill the chip
-  p.tile = tiles_of(m_rows, n_rows, 128, symmetric) * batch >= 256 ? 128 : 64;
-  const int64_t tiles = tiles_of(m_rows, n_rows, p.tile, symmetric) * batch;
+  p.symmetric = symmetric;
+  p.split = 1;
+  p.part_bytes = 0;
   const int pairs = (stages + 1) / 2;
-  int64_t s = 512 / tiles;
-  if (s > 16) s = 16;
-  if (s > pairs / 2) s = pairs / 2;
-  p.split = s < 1 ? 1 : (int)s;
-  p.part_bytes = p.split > 1 ? (size_t)tiles * p.split * p.tile * p.tile * 4 : 0;
+  int64_t tiles;
+  if (big_ok && tiles_of(m_rows, n_rows, 256, false) * batch >= 256) {
+    p.tile = 256;
+    const int64_t all = tiles_of(m_rows, n_rows, 256, false), half = tiles_of(m_rows, n_rows, 256, true);
+    // one triangle alone only where that saves a round of workgroups, one a compute unit
+    if (symmetric && (half * batch + 255) / 256 == (all * batch + 255) / 256 && pairs < 3 * 16) p.symmetric = false;
+    tiles = p.symmetric ? half : all;
+    p.whole = (int)tiles;
+    if (batch == 1) {
+      const int64_t tail = tiles % 256;
+      if (p.symmetric && tiles < 256 && pairs >= 3 * 16) { p.split = 3; p.whole = 0; }
+      else if (tiles > 256 && tail > 0 && tail <= 128 && pairs >= 16) { p.split = 2; p.whole = (int)(tiles - tail); }
+    }
+  } else {
+    p.tile = tiles_of(m_rows, n_rows, 128, symmetric) * batch >= 256 ? 128 : 64;
+    tiles = tiles_of(m_rows, n_rows, p.tile, symmetric);
+    int64_t s = 512 / (tiles * batch);
+    if (s > 16) s = 16;
+    if (s > pairs / 8) s = pairs / 8;
+    p.split = s < 1 ? 1 : (int)s;
+    p.whole = p.split > 1 ? 0 : (int)tiles;
+  }
+  if (p.split > 1) p.part_bytes = (size_t)(tiles - p.whole) * batch * p.split * p.tile * p.tile * 4;
   (void)kind; (void)epi;
   return p;
 }
@@ -392,6 +330,11 @@ TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, 
 namespace {
 template <int KIND, bool KCA, int EPI>
 hipError_t launch_any(const TileArgs& a, const TilePlan& plan, hipStream_t st) {
+  if (plan.tile == 256) {
+    const hipError_t e = launch_tiles_256((TileKind)KIND, (TileEpi)EPI, a, st);
+    const int64_t tiles = tiles_of(a.m_rows, a.n_rows, 256, a.symmetric);
+    return e != hipSuccess || a.whole == tiles ? e : launch_finish<256, EPI>(a, tiles, st);
+  }
   // (64 KiB of LDS either way, two workgroups a compute unit)
   return plan.tile == 128 ? launch<KIND, KCA, 128, 2, EPI>(a, st) : launch<KIND, KCA, 64, 4, EPI>(a, st);
 }
@@ -400,6 +343,8 @@ hipError_t launch_any(const TileArgs& a, const TilePlan& plan, hipStream_t st) {
 hipError_t launch_tiles(TileKind kind, TileEpi epi, const TileArgs& a0, const TilePlan& plan, hipStream_t st) {
   TileArgs a = a0;
   a.split = plan.split;
+  a.whole = plan.whole;
+  a.symmetric = plan.symmetric;
   if (kind == KIND_MX4) return launch_any<KIND_MX4, true, EPI_OUT>(a, plan, st);
   switch (epi) {
     case EPI_GRAM: return launch_any<KIND_F16, true, EPI_GRAM>(a, plan, st);

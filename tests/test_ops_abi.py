@@ -77,7 +77,7 @@ def test_quantize_and_dequantize_refuse(ops):
 
 def test_products_refuse(ops):
     L = ops.lib()
-    n, k, m = 200, 4096, 200
+    n, k, m = 200, 16384, 200
     need = L.gecc_mx4_gemm_workspace(n, k, m)
     assert need > 0                                     # few tiles: k is shared out
     gemm = [n, k, m, OK, OK, OK, OK, OK, 0, m, OK, need, None]

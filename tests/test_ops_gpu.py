@@ -132,7 +132,7 @@ def _check_product(c, a, b, bf16_out):
 
 
 SIZES = [(1, 1, 1), (1, 32, 16), (2, 33, 17), (16, 512, 64), (17, 500, 100), (33, 777, 130), (64, 1024, 15), (65, 256, 63), (66, 257, 65), (128, 100, 128),
-         (129, 1500, 300), (300, 4096, 70), (1000, 777, 1100), (2049, 600, 2050)]
+         (129, 1500, 300), (300, 4096, 70), (130, 16384, 140), (1000, 777, 1100), (2049, 600, 2050)]
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])
