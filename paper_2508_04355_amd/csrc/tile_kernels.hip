@@ -36,10 +36,9 @@ constexpr int THREADS = 256;
 template <bool KC, int T>
 struct TileOperand {
   static constexpr int NV = T * 128 / (THREADS * 16);     // DMA instructions of a wavefront per stage
-  const uint8_t* base;
+  const uint8_t* base;          // of the next stage to be loaded
   int64_t step;                 // bytes from stage to stage
-  int64_t left;                 // bytes from `base` to the end of the operand
-  unsigned voff[NV];
+  unsigned voff[NV];            // (of places beyond the operand: OOB, which reads zero)
   int frag[T / 32];
 
   // place of 16-byte unit p of k-row `krow` in the LDS row (and the other way round): a transposing read takes 32 bytes of
@@ -53,7 +52,6 @@ struct TileOperand {
     if (KC) {
       base = P + (int64_t)r0 * ld + (int64_t)stage0 * 128;
       step = 128;
-      left = rows > r0 ? (int64_t)(rows - r0) * ld - (int64_t)stage0 * 128 : 0;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int s = (wave * NV + i) * 64 + lane, row = s >> 3, c = (s & 7) ^ ((row >> 1) & 7);
@@ -67,7 +65,6 @@ struct TileOperand {
     } else {
       base = P + (int64_t)stage0 * 64 * ld + (int64_t)r0 * 2;
       step = 64 * ld;
-      left = (int64_t)(rows - stage0 * 64) * ld - (int64_t)r0 * 2;      // (rows: the valid k)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int s = (wave * NV + i) * 64 + lane, krow = s / (T / 8), u = unit(krow, s % (T / 8));
@@ -81,13 +78,11 @@ struct TileOperand {
       }
     }
   }
-  // stage number t (from the range's first) into the LDS region at `lds`
-  __device__ __forceinline__ void issue(unsigned lds, int wave_u, int t) const {
-    const int64_t off = (int64_t)t * step, rest = left - off;
-    const i32x4_t rsrc = make_rsrc(base + off, rest <= 0 ? 0u : rest > 0x7fffffff ? 0x7fffffffu : (unsigned)rest);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) dma16(lds + (wave_u * NV + i) * 1024, voff[i], rsrc, 0);
+  // instruction i of the next stage's loads into the LDS region at `lds`; advance() when all of them are out
+  __device__ __forceinline__ void issue(unsigned lds, int wave_u, int i) const {
+    dma16(lds + (wave_u * NV + i) * 1024, voff[i], make_rsrc(base, 0x7fffffffu), 0);
   }
+  __device__ __forceinline__ void advance() { base += step; }
   // the 16 bytes a lane of fragment i (16 rows), instruction ks (0, 1) of the stage
   __device__ __forceinline__ s16x8_t fragment(const char* region, int i, int ks) const {
     if (KC) return *reinterpret_cast<const s16x8_t*>(region + (frag[i] ^ (ks << 6)));
@@ -98,6 +93,23 @@ struct TileOperand {
   }
 };
 
+// f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>), in order
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    static_for<N, I + 1>(f);
+  }
+}
+
+// waits until at most `behind` (0 .. B) stages of PER instructions each are pending
+template <int PER, int B>
+__device__ __forceinline__ void wait_stages(int behind) {
+  if constexpr (B == 0) wait_vm<0>();
+  else if (behind >= B) wait_vm<B * PER>();
+  else wait_stages<PER, B - 1>(behind);
+}
+
 template <int T>
 __device__ __forceinline__ void tile_at(const TileArgs& a, int t, int& tm, int& tn) {
   if (a.symmetric) { triangle(t, tm, tn); return; }
@@ -106,7 +118,7 @@ __device__ __forceinline__ void tile_at(const TileArgs& a, int t, int& tm, int& 
   tn = t / ntm;
 }
 
-// RING: stages of LDS, RING - 1 of them on their way while one is in use
+// RING: stages of LDS
 template <int KIND, bool KCA, int T, int RING, int EPI>
 __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_out) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -135,14 +147,12 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
   // scales: instruction number `wave` of the 2 T / 64 of a pair (64 rows each); wavefronts beyond them repeat the last
   const uint8_t* sbase = nullptr;
   unsigned svoff = 0, slds = 0;
-  int64_t sleft = 0;
   if (KIND == KIND_MX4) {
     const int q = min(wave_u, 2 * T / 64 - 1), per = T / 64;
     const bool is_b = q >= per;
     const int row = (is_b ? q - per : q) * 64 + lane;
     const int64_t units = pairs, row0 = is_b ? c0 : r0, rows16 = ((is_b ? a.n_rows : a.m_rows) + 15) / 16;
     sbase = (is_b ? a.scale_b : a.scale_a) + (row0 / 16 * units + first / 2) * 256;
-    sleft = (rows16 - row0 / 16) * units * 256 - (int64_t)(first / 2) * 256;
     svoff = (unsigned)((row >> 4) * units * 256 + (row & 15) * 16);
     if (row0 / 16 + (row >> 4) >= rows16) svoff = OOB;
     slds = (is_b ? SCALES : 0) + (unsigned)(is_b ? q - per : q) * 1024;
@@ -155,71 +165,106 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
     for (int j = 0; j < F; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  auto issue = [&](int t) {
+  constexpr int NA = TileOperand<KCA, T>::NV, NB = TileOperand<true, T>::NV, PER = NA + NB;
+  // instruction d of stage t's loads (a pair's scales go out with its first stage's first)
+  auto issue_one = [&](int t, int d, bool even) {
     const unsigned at = lds0 + (t & (RING - 1)) * SLOT;
-    if (KIND == KIND_MX4 && (t & 1) == 0) {
-      const int64_t off = (int64_t)(t >> 1) * 256, rest = sleft - off;
-      const i32x4_t rsrc = make_rsrc(sbase + off, rest <= 0 ? 0u : rest > 0x7fffffff ? 0x7fffffffu : (unsigned)rest);
-      dma16(lds0 + RING * SLOT + ((t >> 1) & (RING / 2 - 1)) * 2 * SCALES + slds, svoff, rsrc, 0);
+    if (KIND == KIND_MX4 && even && d == 0) {
+      dma16(lds0 + RING * SLOT + ((t >> 1) & (RING / 2 - 1)) * 2 * SCALES + slds, svoff, make_rsrc(sbase, 0x7fffffffu), 0);
+      sbase += 256;
     }
-    oa.issue(at, wave_u, t);
-    ob.issue(at + STAGE, wave_u, t);
+    if (d < NA) oa.issue(at, wave_u, d);
+    else ob.issue(at + STAGE, wave_u, d - NA);
+    if (d == PER - 1) { oa.advance(); ob.advance(); }
   };
-  int sa[F], sb[F];
+  auto load_all = [&](int t) {
 #pragma unroll
-  for (int i = 0; i < F; ++i) sa[i] = sb[i] = 0;
-  auto multiply = [&](int t, auto odd_c) {
-    constexpr bool ODD = decltype(odd_c)::value;
+    for (int d = 0; d < PER; ++d) issue_one(t, d, (t & 1) == 0);
+  };
+  // Software pipeline: while the matrix instructions of stage t run, the fragments of stage t + 1 come out of LDS into the
+  // other of two sets, and the loads of stage t + RING go out into the slot of stage t (the barrier before says that
+  // everyone has its fragments).  Reads and loads are dealt out between the matrix instructions: the address unit takes a
+  // load instruction in 16 cycles, so that those of four wavefronts in a row hold each of them up as long as its matrix
+  // instructions last (128 x 128 tiles: 1300 cycles a stage with loads, reads and products one after the other, 870 so).
+  s16x8_t fa[2][2][F], fb[2][2][F];                    // [set][instruction of the stage]
+  int sa[F], sb[F], sa_next[F], sb_next[F];             // scales of two stages
+#pragma unroll
+  for (int i = 0; i < F; ++i) sa[i] = sb[i] = sa_next[i] = sb_next[i] = 0;
+  constexpr int READS = 4 * F, PRODUCTS = 2 * F * F;
+  auto fetch_one = [&](int t, auto set_c, auto r_c) {
+    constexpr int SET = decltype(set_c)::value, R = decltype(r_c)::value, KS = R / (2 * F), I = R % (2 * F);
     const char* ra = smem + (t & (RING - 1)) * SLOT;
-    const char* rb = ra + STAGE;
-    if (KIND == KIND_MX4 && !ODD) {
-      const char* rs = smem + RING * SLOT + ((t >> 1) & (RING / 2 - 1)) * 2 * SCALES;
+    if constexpr (I < F) fa[SET][KS][I] = oa.fragment(ra, I, KS);
+    else fb[SET][KS][I - F] = ob.fragment(ra + STAGE, I - F, KS);
+  };
+  auto fetch_scales = [&](int t) {                      // of an even stage and the one behind it
+    const char* rs = smem + RING * SLOT + ((t >> 1) & (RING / 2 - 1)) * 2 * SCALES;
 #pragma unroll
-      for (int i = 0; i < F; ++i) {
-        sa[i] = *reinterpret_cast<const int*>(rs + (wr * (T / 2) + i * 16 + l16) * 16 + g * 4);
-        sb[i] = *reinterpret_cast<const int*>(rs + SCALES + (wc * (T / 2) + i * 16 + l16) * 16 + g * 4);
-      }
-    }
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      s16x8_t fa[F], fb[F];
-#pragma unroll
-      for (int i = 0; i < F; ++i) fa[i] = oa.fragment(ra, i, ks);
-#pragma unroll
-      for (int j = 0; j < F; ++j) fb[j] = ob.fragment(rb, j, ks);
-#pragma unroll
-      for (int i = 0; i < F; ++i)
-#pragma unroll
-        for (int j = 0; j < F; ++j) {
-          if (KIND == KIND_F16) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, fa[i]), __builtin_bit_cast(f16x8_t, fb[j]), acc[i][j], 0, 0, 0);
-          } else {
-            const i32x4_t xa = __builtin_bit_cast(i32x4_t, fa[i]), xb = __builtin_bit_cast(i32x4_t, fb[j]);
-            const i32x8_t va = {xa[0], xa[1], xa[2], xa[3], 0, 0, 0, 0}, vb = {xb[0], xb[1], xb[2], xb[3], 0, 0, 0, 0};
-            // (the byte of the scale registers, 2 ODD + ks, is a constant of the instruction)
-            if (ks == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(va, vb, acc[i][j], 4, 4, ODD ? 2 : 0, sa[i], ODD ? 2 : 0, sb[j]);
-            else         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(va, vb, acc[i][j], 4, 4, ODD ? 3 : 1, sa[i], ODD ? 3 : 1, sb[j]);
-          }
-        }
+    for (int i = 0; i < F; ++i) {
+      sa_next[i] = *reinterpret_cast<const int*>(rs + (wr * (T / 2) + i * 16 + l16) * 16 + g * 4);
+      sb_next[i] = *reinterpret_cast<const int*>(rs + SCALES + (wc * (T / 2) + i * 16 + l16) * 16 + g * 4);
     }
   };
-  // Stage t has landed when no more instructions are pending than the stages behind it have (a stage's scales go out first)
-  constexpr int PER = TileOperand<KCA, T>::NV + TileOperand<true, T>::NV;
-  auto step = [&](int t, auto odd_c) {
-    const int behind = min(RING - 2, count - 1 - t);
-    if (RING > 3 && behind == 2) wait_vm<(RING > 3 ? 2 : 0) * PER>();
-    else if (RING > 2 && behind == 1) wait_vm<(RING > 2 ? 1 : 0) * PER>();
-    else wait_vm<0>();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wavefront's reads of stage t - 1 are back
-    __builtin_amdgcn_s_barrier();                        // stage t complete for everyone, the slot of stage t - 1 free
+  auto product = [&](auto set_c, auto n_c) {
+    constexpr int SET = decltype(set_c)::value, N = decltype(n_c)::value, KS = N / (F * F), I = N / F % F, J = N % F;
+    if constexpr (KIND == KIND_F16) {
+      acc[I][J] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, fa[SET][KS][I]), __builtin_bit_cast(f16x8_t, fb[SET][KS][J]), acc[I][J], 0, 0, 0);
+    } else {
+      const i32x4_t xa = __builtin_bit_cast(i32x4_t, fa[SET][KS][I]), xb = __builtin_bit_cast(i32x4_t, fb[SET][KS][J]);
+      const i32x8_t va = {xa[0], xa[1], xa[2], xa[3], 0, 0, 0, 0}, vb = {xb[0], xb[1], xb[2], xb[3], 0, 0, 0, 0};
+      constexpr int BYTE = 2 * SET + KS;                // of the scale words
+      acc[I][J] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(va, vb, acc[I][J], 4, 4, BYTE, sa[I], BYTE, sb[J]);
+    }
+  };
+  // at most `behind` stages asked for later than the one that is needed are pending; then everyone's part of it has landed
+  auto landed = [&](int behind) {
+    wait_stages<PER, RING - 1>(behind);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wavefront's reads of the stage before are back
+    __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (t + RING - 1 < count) issue(t + RING - 1);
-    multiply(t, odd_c);
   };
-  for (int t = 0; t < min(RING - 1, count); ++t) issue(t);
-  for (int t = 0; t < count; t += 2) {
-    step(t, std::false_type{});
-    if (t + 1 < count) step(t + 1, std::true_type{});
+  // stage t; MORE: with stage t + RING to be loaded between the products.  (Behind the last stage the reads take a slot that
+  // nobody filled: in range, never used.)
+  auto step = [&](int t, auto set_c, auto more_c) {
+    constexpr int SET = decltype(set_c)::value;
+    constexpr bool MORE = decltype(more_c)::value;
+    if (KIND == KIND_MX4 && SET == 0) {
+#pragma unroll
+      for (int i = 0; i < F; ++i) { sa[i] = sa_next[i]; sb[i] = sb_next[i]; }
+    }
+    landed(min(RING - 2, count - 2 - t));
+    if (!MORE && t + RING < count) load_all(t + RING);       // (an odd last stage)
+    if (KIND == KIND_MX4 && SET == 1) fetch_scales(t + 1);
+    static_for<PRODUCTS>([&](auto n_c) {
+      constexpr int N = decltype(n_c)::value;
+      product(set_c, n_c);
+      __builtin_amdgcn_sched_barrier(0);
+      // reads over the first half of the products, loads over all of them
+      constexpr int r0 = 2 * N * READS / PRODUCTS, r1 = 2 * (N + 1) * READS / PRODUCTS;
+      if constexpr (r0 < READS)
+        static_for<(r1 < READS ? r1 : READS) - r0>([&](auto q_c) {
+          fetch_one(t + 1, std::integral_constant<int, 1 - SET>{}, std::integral_constant<int, r0 + decltype(q_c)::value>{});
+        });
+      constexpr int d0 = (N * PER + PRODUCTS / 2) / PRODUCTS, d1 = ((N + 1) * PER + PRODUCTS / 2) / PRODUCTS;
+      if constexpr (MORE)
+        static_for<d1 - d0>([&](auto q_c) { issue_one(t + RING, d0 + decltype(q_c)::value, SET == 0); });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  const std::integral_constant<int, 0> even{};
+  const std::integral_constant<int, 1> odd{};
+  for (int t = 0; t < min(RING, count); ++t) load_all(t);
+  landed(min(RING, count) - 1);
+  if (KIND == KIND_MX4) fetch_scales(0);
+  static_for<READS>([&](auto r_c) { fetch_one(0, even, r_c); });
+  int t = 0;
+  for (; t + RING + 1 < count; t += 2) {
+    step(t, even, std::true_type{});
+    step(t + 1, odd, std::true_type{});
+  }
+  for (; t < count; t += 2) {
+    step(t, even, std::false_type{});
+    if (t + 1 < count) step(t + 1, odd, std::false_type{});
   }
 
   if (a.split > 1) {
@@ -276,7 +321,7 @@ hipError_t launch_finish(const TileArgs& a, int64_t tiles, hipStream_t st) {
 
 template <int KIND, bool KCA, int T, int RING, int EPI>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
-  static_assert(RING == 2 || RING == 4, "the waits of tile_kernel");
+  static_assert(RING % 2 == 0 && (RING & (RING - 1)) == 0, "slots of stages, and of their scales, by number");
   const int64_t tiles = tiles_of(a.m_rows, a.n_rows, T, a.symmetric);
   if (tiles > 0x7fffffff || a.batch > 65535) return hipErrorInvalidValue;
   constexpr int lds = RING * 2 * T * 128 + (KIND == KIND_MX4 ? RING / 2 * 2 * T * 16 : 0);
@@ -294,37 +339,62 @@ hipError_t launch(const TileArgs& a, hipStream_t st) {
 
 }  // namespace
 
+namespace {
+// Times (us) as fitted to measurements, both kinds of operand (a stage is 128 bytes of k a row, the same work for both): what
+// a round of workgroups takes beside its stages, and a stage with one workgroup a compute unit and with two.
+//                            measured / by this fit
+//   4-bit  512 x 4096 x 4096      tiles of 64 11.6 / 12   of 128 12.7 / 14   (128 workgroups)
+//   4-bit  2048 x 4096 x 4096     64 36.6 / 38   128 19.9 / 22   256 27.8 / 34
+//   4-bit  4096^3                 128 38.6 / 40   256 34.9 / 34
+//   fp16   X X^T, 2048 x 4096     64 41.9 / 44   128 35.4 / 38, in three ranges 34 / 39
+//   fp16   P X, 4096 x 14336      128 423 / 424   256 360 / 369
+double rounds_of(int64_t groups, int at_once) {
+  const int64_t full = groups / at_once, rest = groups % at_once;
+  return (double)full + (rest == 0 ? 0.0 : 2 * rest <= at_once && full > 0 ? 0.6 : 1.0);
+}
+double tile_time(int tile, int64_t groups, double stages, bool mirrored) {
+  if (tile == 256) return 3.0 + (double)((groups + 255) / 256) * (9.0 + 1.35 * stages);
+  const double fixed = (tile == 128 ? 4.5 : 2.5) + (mirrored ? (tile == 128 ? 4.0 : 0.5) : 0.0);
+  if (groups <= 256) return 3.0 + fixed + stages * (tile == 128 ? 0.42 : 0.2);
+  return 3.0 + rounds_of(groups, 512) * (fixed + stages * (tile == 128 ? 0.87 : 0.39));
+}
+double finish_time(size_t part_bytes) { return part_bytes ? 4.5 + 0.25e-6 * (double)part_bytes : 0.0; }
+constexpr size_t MOST_PART_BYTES = (size_t)128 << 20;
+}  // namespace
+
 TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, int stages, int batch, bool symmetric, bool big_ok) {
-  TilePlan p;
-  p.symmetric = symmetric;
-  p.split = 1;
-  p.part_bytes = 0;
-  const int pairs = (stages + 1) / 2;
-  int64_t tiles;
-  if (big_ok && tiles_of(m_rows, n_rows, 256, false) * batch >= 256) {
-    p.tile = 256;
-    const int64_t all = tiles_of(m_rows, n_rows, 256, false), half = tiles_of(m_rows, n_rows, 256, true);
-    // one triangle alone only where that saves a round of workgroups, one a compute unit
-    if (symmetric && (half * batch + 255) / 256 == (all * batch + 255) / 256 && pairs < 3 * 16) p.symmetric = false;
-    tiles = p.symmetric ? half : all;
-    p.whole = (int)tiles;
-    if (batch == 1) {
-      const int64_t tail = tiles % 256;
-      if (p.symmetric && tiles < 256 && pairs >= 3 * 16) { p.split = 3; p.whole = 0; }
-      else if (tiles > 256 && tail > 0 && tail <= 128 && pairs >= 16) { p.split = 2; p.whole = (int)(tiles - tail); }
-    }
-  } else {
-    p.tile = tiles_of(m_rows, n_rows, 128, symmetric) * batch >= 256 ? 128 : 64;
-    tiles = tiles_of(m_rows, n_rows, p.tile, symmetric);
-    int64_t s = 512 / (tiles * batch);
-    if (s > 16) s = 16;
-    if (s > pairs / 8) s = pairs / 8;
-    p.split = s < 1 ? 1 : (int)s;
-    p.whole = p.split > 1 ? 0 : (int)tiles;
+  (void)kind;
+  TilePlan best{};
+  double least = 1e300;
+  const int twos = (stages + 1) / 2;                 // ranges are whole pairs of stages
+  auto consider = [&](int tile, int split, int64_t whole, bool triangle_only) {
+    const int64_t tiles = tiles_of(m_rows, n_rows, tile, triangle_only);
+    if (split > twos || whole > tiles) return;
+    const size_t part = split > 1 ? (size_t)(tiles - whole) * batch * split * tile * tile * 4 : 0;
+    if (part > MOST_PART_BYTES) return;
+    double t = finish_time(part);
+    if (whole > 0 && split > 1) t += tile_time(tile, whole * batch, stages, triangle_only) - 3.0 + tile_time(tile, (tiles - whole) * split, (double)stages / split, false);
+    else t += tile_time(tile, tiles * batch * split, (double)stages / split, triangle_only && split == 1);
+    if (t >= least) return;
+    least = t;
+    best.tile = tile;
+    best.split = split;
+    best.whole = split > 1 ? (int)whole : (int)tiles;
+    best.symmetric = triangle_only;
+    best.part_bytes = part;
+  };
+  if (big_ok) {
+    if (!symmetric || epi == EPI_POLY || epi == EPI_GRAM) consider(256, 1, 0, false);
+    if (symmetric) for (int s = 1; s <= 8; ++s) consider(256, s, 0, true);
+    // a last round of at most half the compute units: two workgroups a tile
+    const int64_t tiles = tiles_of(m_rows, n_rows, 256, false), tail = tiles % 256;
+    if (batch == 1 && tiles > 256 && tail > 0 && tail <= 128) consider(256, 2, tiles - tail, false);
   }
-  if (p.split > 1) p.part_bytes = (size_t)(tiles - p.whole) * batch * p.split * p.tile * p.tile * 4;
-  (void)kind; (void)epi;
-  return p;
+  for (const int tile : {128, 64}) {
+    const int64_t groups = tiles_of(m_rows, n_rows, tile, symmetric) * batch;
+    for (int s = 1; s <= 16 && (s == 1 || groups * s <= 1024); ++s) consider(tile, s, 0, symmetric);
+  }
+  return best;
 }
 
 namespace {
@@ -335,8 +405,10 @@ hipError_t launch_any(const TileArgs& a, const TilePlan& plan, hipStream_t st) {
     const int64_t tiles = tiles_of(a.m_rows, a.n_rows, 256, a.symmetric);
     return e != hipSuccess || a.whole == tiles ? e : launch_finish<256, EPI>(a, tiles, st);
   }
-  // (64 KiB of LDS either way, two workgroups a compute unit)
-  return plan.tile == 128 ? launch<KIND, KCA, 128, 2, EPI>(a, st) : launch<KIND, KCA, 64, 4, EPI>(a, st);
+  // 64 KiB of LDS, two workgroups a compute unit; tiles of 128 that are no more than compute units have twice that
+  const int64_t groups = tiles_of(a.m_rows, a.n_rows, plan.tile, a.symmetric) * a.split * a.batch;
+  if (plan.tile == 128) return groups <= 256 ? launch<KIND, KCA, 128, 4, EPI>(a, st) : launch<KIND, KCA, 128, 2, EPI>(a, st);
+  return launch<KIND, KCA, 64, 4, EPI>(a, st);
 }
 }  // namespace
 
