@@ -87,6 +87,7 @@ struct OrthPlan {
   int nparts;
   int chunk;                      // batch items that go through all steps together
   TilePlan gram, poly, update;
+  size_t q;                       // matrices of up to 64 rows
   size_t parts, x[2], lo[2], gram_at, poly_at, part, total;
   OrthSteps steps;
 };
@@ -153,12 +154,19 @@ bool orth_plan(const gecc_orth_params* p, OrthPlan* o) {
   o->l = o->tall ? p->rows : p->cols;
   o->sp = align_up(o->s, 64);
   o->lp = align_up(o->l, 64);
+  o->total = 0;
+  if (orth_small_ok(o->s, o->l)) return true;
+  if (o->s <= ORTH_NARROW) {
+    o->nparts = orth_narrow_parts(o->l, p->batch);
+    o->parts = 0;
+    o->q = align_up(orth_narrow_part_bytes(o->s, o->nparts, p->batch), 256);
+    o->total = o->q + align_up(orth_narrow_q_bytes(o->s, p->batch), 256);
+    return true;
+  }
   const int64_t elements = (int64_t)p->rows * p->cols;
   // a workgroup per 2048 elements (eight a thread), up to four a compute unit in all
   const int64_t parts = (elements + 2047) / 2048, most = p->batch >= ORTH_PARTS ? 1 : ORTH_PARTS / p->batch;
   o->nparts = (int)(parts > most ? most : parts);
-  o->total = 0;
-  if (orth_small_ok(o->s, o->l)) return true;
   // X in its two halves, twice, S and P of the items of a chunk: what the steps read and write stays in the 256 MiB memory-side
   // cache (512 x 512 bf16, 256 items: 3673 us all at once, 2287 in chunks of 64 together with the epilogue by rows)
   const int64_t item = 4 * o->sp * o->lp * 2 + 2 * (int64_t)o->s * o->sp * 2;
@@ -402,6 +410,7 @@ int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_
   prep.s = o.s; prep.l = o.l; prep.sp = o.sp; prep.lp = o.lp; prep.tall = o.tall;
   prep.x_scale = o.steps.sx[0];
   if (orth_small_ok(o.s, o.l)) return hip_rc(launch_orth_small(prep, dev_O, o.steps, st));
+  if (o.s <= ORTH_NARROW) return hip_rc(launch_orth_narrow(prep, dev_O, reinterpret_cast<float*>(ws + o.q), st));
   hipError_t e = launch_orth_norm(prep, st);
   if (e != hipSuccess) return hip_rc(e);
   if (p->steps == 0) return hip_rc(launch_orth_store(prep, dev_O, st));

@@ -108,6 +108,12 @@ hipError_t launch_orth_start(const OrthPrepArgs& a, hipStream_t st);     // X
 // all of it in one launch, for matrices of up to 128 x 256
 bool orth_small_ok(int s, int l);
 hipError_t launch_orth_small(const OrthPrepArgs& a, void* out, const OrthSteps& steps, hipStream_t st);
+// matrices with a shorter side of up to 64 (orth_narrow_kernels.hip): `parts` holds orth_narrow_part_bytes, q orth_narrow_q_bytes
+constexpr int ORTH_NARROW = 64;
+int orth_narrow_parts(int l, int batch);
+size_t orth_narrow_part_bytes(int s, int nparts, int batch);
+size_t orth_narrow_q_bytes(int s, int batch);
+hipError_t launch_orth_narrow(const OrthPrepArgs& a, void* out, float* q, hipStream_t st);
 // O = scale * X where there are no steps
 hipError_t launch_orth_store(const OrthPrepArgs& a, void* out, hipStream_t st);
 

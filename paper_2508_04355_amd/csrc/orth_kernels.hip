@@ -4,6 +4,7 @@
 #include "ops_internal.h"
 #include "ops_device.h"
 #include "lds_limit.h"
+#include "orth_device.h"
 
 namespace gecc {
 namespace {
@@ -11,14 +12,6 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 
 constexpr int NORM_PIECES = 4;
-
-template <bool BF16G, bool VEC>
-__device__ __forceinline__ void load_g(const OrthPrepArgs& a, int b, int64_t row, int c, bool ok, float (&g)[8]) {
-  load8<!BF16G, VEC>(static_cast<const char*>(a.G) + (int64_t)b * a.p.stride_g * (BF16G ? 2 : 4), row * a.p.ld_g + c, c, a.p.cols, ok, g);
-}
-
-// U from G and the momentum after its update
-__device__ __forceinline__ float update_of(const OrthPrepArgs& a, float g, float m) { return a.p.nesterov ? fmaf(a.p.mu, m, g) : m; }
 
 // M <- mu M + G; the sum of U^2 of this workgroup's pieces, in fp64 (squares of fp32 neither overflow nor vanish there)
 template <bool BF16G, bool VEC>
@@ -185,6 +178,18 @@ template <int PITCH>
 __device__ __forceinline__ f16x8_t row_fragment(const char* m, int row, int chunk) {
   return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const s16x8_t*>(m + row * PITCH + (swizzle(row, chunk) << 4)));
 }
+// 16 columns from `col` on, rows `row` .. `row` + 31
+template <int PITCH>
+__device__ __forceinline__ f16x8_t column_fragment(const char* m, int row, int col) {
+  const int lane = threadIdx.x & 63;
+  const int r = row + 8 * (lane >> 4) + ((lane >> 2) & 3), c = col + (lane & 3) * 4;
+  const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(m + r * PITCH + (swizzle(r, c >> 3) << 4) + (c & 7) * 2));
+  const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(m + (r + 4) * PITCH + (swizzle(r + 4, c >> 3) << 4) + (c & 7) * 2));
+  return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// Matrices of up to 64 rows: P X from both halves of both (three products): with few singular values the roundings of an
+// update do not average out (16 x 16 noise: up to 2.3e-3 from one half of each, 1.3e-3), and there is LDS for it
+constexpr bool small_halves(int sp) { return sp <= 64; }
 // four fp16 values of row `row` from column `col` (a multiple of 4) on
 template <int PITCH>
 __device__ __forceinline__ void put4(char* m, int row, int col, const float (&x)[4]) {
@@ -200,6 +205,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
   constexpr int UP = LP + 1;                       // fp32 U in LDS: [SP][UP], before anything else lies there
   constexpr int XPITCH = LP * 2 < 256 ? 256 : LP * 2, SPITCH = 256;
   constexpr int FI = LP / 32, FJ = SP / 64, GI = SP / 32;     // 16 x 16 blocks of a wavefront: update, gram and polynomial
+  constexpr bool TWO_HALVES = small_halves(SP);
   const OrthPrepArgs& o = a.prep;
   const gecc_orth_params& p = o.p;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
@@ -272,13 +278,23 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
   __syncthreads();
   char* X = smem;
   char* S = smem + SP * XPITCH;
+  char* X_lo = S + SP * SPITCH;                   // TWO_HALVES
+  char* S_lo = X_lo + SP * XPITCH;
   constexpr int KL = LP / 32, KS = SP / 32;        // (zeros beyond the matrix)
   for (int t = 0; t < p.steps; ++t) {
     const float sx = a.steps.sx[t], ss = a.steps.ss[t], sp = a.steps.sp[t], fold = a.steps.fold[t];
 #pragma unroll
     for (int i = 0; i < FI; ++i)
 #pragma unroll
-      for (int j = 0; j < FJ; ++j) put4<XPITCH>(X, (FJ * wj + j) * 16 + l16, (FI * wi + i) * 16 + 4 * g, x[i][j]);
+      for (int j = 0; j < FJ; ++j) {
+        put4<XPITCH>(X, (FJ * wj + j) * 16 + l16, (FI * wi + i) * 16 + 4 * g, x[i][j]);
+        if (TWO_HALVES) {
+          float y[4];
+#pragma unroll
+          for (int v = 0; v < 4; ++v) y[v] = x[i][j][v] - (float)(_Float16)x[i][j][v];
+          put4<XPITCH>(X_lo, (FJ * wj + j) * 16 + l16, (FI * wi + i) * 16 + 4 * g, y);
+        }
+      }
     __syncthreads();
     // S (i, j blocks: wi, wj); its row j gets the values of its column j: S is symmetric
     f32x4_t gram[GI][FJ], poly[GI][FJ];
@@ -337,6 +353,11 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
           if ((GI * wi + i) * 16 + 4 * g + v == (FJ * wj + j) * 16 + l16) y[v] += eye;
         }
         put4<SPITCH>(S, (FJ * wj + j) * 16 + l16, (GI * wi + i) * 16 + 4 * g, y);
+        if (TWO_HALVES) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) y[v] -= (float)(_Float16)y[v];
+          put4<SPITCH>(S_lo, (FJ * wj + j) * 16 + l16, (GI * wi + i) * 16 + 4 * g, y);
+        }
       }
     __syncthreads();
     const bool last = t + 1 == p.steps;
@@ -348,18 +369,25 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
       for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      f16x8_t fb[FJ];
+      f16x8_t fb[FJ], fb_lo[FJ];
 #pragma unroll
-      for (int j = 0; j < FJ; ++j) fb[j] = row_fragment<SPITCH>(S, (FJ * wj + j) * 16 + l16, k * 4 + g);
-      const int q4 = (lane & 3) * 4, row = k * 32 + 8 * g + ((lane >> 2) & 3);
+      for (int j = 0; j < FJ; ++j) {
+        fb[j] = row_fragment<SPITCH>(S, (FJ * wj + j) * 16 + l16, k * 4 + g);
+        if (TWO_HALVES) fb_lo[j] = row_fragment<SPITCH>(S_lo, (FJ * wj + j) * 16 + l16, k * 4 + g);
+      }
 #pragma unroll
       for (int i = 0; i < FI; ++i) {
-        const int col = (FI * wi + i) * 16 + q4;
-        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(X + row * XPITCH + (swizzle(row, col >> 3) << 4) + (col & 7) * 2));
-        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(X + (row + 4) * XPITCH + (swizzle(row + 4, col >> 3) << 4) + (col & 7) * 2));
-        const f16x8_t fa = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        const f16x8_t fa = column_fragment<XPITCH>(X, k * 32, (FI * wi + i) * 16);
 #pragma unroll
         for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa, fb[j], acc[i][j], 0, 0, 0);
+        if (TWO_HALVES) {
+          const f16x8_t fa_lo = column_fragment<XPITCH>(X_lo, k * 32, (FI * wi + i) * 16);
+#pragma unroll
+          for (int j = 0; j < FJ; ++j) {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa_lo, fb[j], acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa, fb_lo[j], acc[i][j], 0, 0, 0);
+          }
+        }
       }
     }
 #pragma unroll
@@ -396,16 +424,9 @@ __global__ __launch_bounds__(SMALL_THREADS) void orth_small_kernel(OrthSmallArgs
     }
 }
 
-bool vectors_ok(const OrthPrepArgs& a) {
-  const int64_t es = a.p.dtype == GECC_F32 ? 4 : 2;
-  if (reinterpret_cast<uintptr_t>(a.G) % 16 || a.p.ld_g * es % 16 || (a.p.batch > 1 && a.p.stride_g * es % 16)) return false;
-  if (!a.M) return true;
-  return reinterpret_cast<uintptr_t>(a.M) % 16 == 0 && a.p.ld_m % 4 == 0 && (a.p.batch == 1 || a.p.stride_m % 4 == 0);
-}
-
 template <int SP, int LP>
 hipError_t small(const OrthSmallArgs& a, hipStream_t st) {
-  constexpr int u_bytes = SP * (LP + 1) * 4 / 8 * 8 + 8 + 64, x_bytes = SP * (LP * 2 < 256 ? 256 : LP * 2) + SP * 256;
+  constexpr int u_bytes = SP * (LP + 1) * 4 / 8 * 8 + 8 + 64, x_bytes = (SP * (LP * 2 < 256 ? 256 : LP * 2) + SP * 256) * (small_halves(SP) ? 2 : 1);
   constexpr int lds = u_bytes > x_bytes ? u_bytes : x_bytes;
   const bool bf16 = a.prep.p.dtype == GECC_BF16, vec = vectors_ok(a.prep);
   auto kern = bf16 ? (vec ? orth_small_kernel<SP, LP, true, true> : orth_small_kernel<SP, LP, true, false>)
@@ -454,9 +475,7 @@ bool orth_small_ok(int s, int l) { return s <= 128 && l <= 256; }
 
 hipError_t launch_orth_small(const OrthPrepArgs& prep, void* out, const OrthSteps& steps, hipStream_t st) {
   if (!orth_small_ok(prep.s, prep.l)) return hipErrorInvalidValue;
-  const int es = prep.p.out_dtype == GECC_F32 ? 4 : 2;
-  const bool vec_out = reinterpret_cast<uintptr_t>(out) % (4 * es) == 0 && prep.p.ld_o % 4 == 0 && (prep.p.batch == 1 || prep.p.stride_o % 4 == 0);
-  const OrthSmallArgs a = {prep, out, vec_out, steps};
+  const OrthSmallArgs a = {prep, out, orth_vec_out(prep, out), steps};
   if (prep.s <= 64) return prep.l <= 128 ? small<64, 128>(a, st) : small<64, 256>(a, st);
   return prep.l <= 128 ? small<128, 128>(a, st) : small<128, 256>(a, st);
 }

@@ -1,0 +1,318 @@
+// The orthogonalised update of matrices whose shorter side s is at most 64 (formulas: gecc_ops.h).
+//
+// X goes through polynomials of S = X X^T, which all commute, so that the steps can be done on s x s matrices alone:
+//   T = a I + b S + c S S,   S <- T S T,   Q <- T Q   (Q = I at first),   O = scale Q X  at the end.
+// The long side is read twice, whatever the number of steps, instead of three times a step.  What that costs is
+// precision: S holds the squares of the singular values, and what a step's rounding adds to the small ones grows by a^2 a
+// step, so S is formed and stepped in fp64 (its products are exact: 24 + 24 bits), on the fp64 matrix instructions.  Three
+// launches: sums of U U^T over ranges of the long side (with the momentum), the steps in one workgroup a matrix, Q X.
+// Bound by: latency for one matrix (64 x 64: eighteen products of 2600 cycles each), memory for long ones.
+// Measured: NARROWFIG
+#include "ops_internal.h"
+#include "ops_device.h"
+#include "lds_limit.h"
+#include "orth_device.h"
+
+namespace gecc {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) double f64x4_t;
+constexpr int LT = 64;                       // elements of the long side of a tile
+constexpr int UP = LT + 1;
+
+__device__ __forceinline__ int block_count(int sp) { return sp / 16 * (sp / 16 + 1) / 2; }
+// block number q of the lower triangle
+__device__ __forceinline__ void block_at(int q, int& bi, int& bj) {
+  bi = q < 1 ? 0 : q < 3 ? 1 : q < 6 ? 2 : 3;
+  bj = q - bi * (bi + 1) / 2;
+}
+
+// A tile of U, [SP][UP] with the short side first, zeros beyond the matrix; STORE: G and M as they come, M updated; else M is the
+// updated one, and U is multiplied by f
+template <int SP, bool BF16G, bool VEC, bool STORE>
+__device__ __forceinline__ void load_tile(const OrthPrepArgs& a, int b, int tile, float f, float* U) {
+  constexpr int PIECES = SP * LT / 8;
+  float* M = a.M ? a.M + (int64_t)b * a.p.stride_m : nullptr;
+#pragma unroll
+  for (int h = 0; h < (PIECES + 255) / 256; ++h) {
+    const int q = h * 256 + threadIdx.x;
+    if (PIECES % 256 != 0 && q >= PIECES) break;
+    const int64_t row = a.tall ? (int64_t)tile * LT + q / (SP / 8) : q / (LT / 8);
+    const int c = a.tall ? q % (SP / 8) * 8 : tile * LT + q % (LT / 8) * 8;
+    const bool ok = row < a.p.rows && c < a.p.cols;
+    float g[8], m[8];
+    load_g<BF16G, VEC>(a, b, row, c, ok, g);
+    if (M) {
+      load8<true, VEC>(M, row * a.p.ld_m + c, c, a.p.cols, ok, m);
+      if (STORE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = fmaf(a.p.mu, m[i], g[i]);
+        if (ok) {
+          float* o = M + row * a.p.ld_m + c;
+          if (VEC && c + 8 <= a.p.cols) {
+            reinterpret_cast<f32x4_t*>(o)[0] = f32x4_t{m[0], m[1], m[2], m[3]};
+            reinterpret_cast<f32x4_t*>(o)[1] = f32x4_t{m[4], m[5], m[6], m[7]};
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (c + i < a.p.cols) o[i] = m[i];
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = update_of(a, g[i], m[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float u = STORE ? g[i] : g[i] * f;
+      if (a.tall) U[(c + i) * UP + q / (SP / 8)] = u;
+      else U[(q / (LT / 8)) * UP + q % (LT / 8) * 8 + i] = u;
+    }
+  }
+}
+
+// sums of U U^T over the tiles blockIdx.x, + gridDim.x, ..: the blocks of the lower triangle, 256 doubles each
+template <int SP, bool BF16G, bool VEC>
+__global__ __launch_bounds__(256) void narrow_gram_kernel(OrthPrepArgs a, int tiles) {
+  constexpr int NI = SP / 16, NB = NI * (NI + 1) / 2;
+  __shared__ float U[SP * UP];
+  __shared__ double red[4 * 256];
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lg = lane >> 4;
+  f64x4_t acc[NB];
+#pragma unroll
+  for (int q = 0; q < NB; ++q) acc[q] = f64x4_t{0.0, 0.0, 0.0, 0.0};
+  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+    load_tile<SP, BF16G, VEC, true>(a, b, t, 1.f, U);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {              // this wavefront's 16 of the 64, four an instruction
+      double x[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) x[i] = (double)U[(16 * i + l16) * UP + wave * 16 + k * 4 + lg];
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j <= i; ++j) acc[i * (i + 1) / 2 + j] = __builtin_amdgcn_mfma_f64_16x16x4f64(x[i], x[j], acc[i * (i + 1) / 2 + j], 0, 0, 0);
+    }
+    __syncthreads();
+  }
+  double* out = a.parts + ((int64_t)b * gridDim.x + blockIdx.x) * (NB * 256);
+#pragma unroll
+  for (int q = 0; q < NB; ++q) {
+    // (these results have row 4 v + lg)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) red[wave * 256 + (4 * v + lg) * 16 + l16] = acc[q][v];
+    __syncthreads();
+    out[q * 256 + tid] = (red[tid] + red[256 + tid]) + (red[512 + tid] + red[768 + tid]);
+    __syncthreads();
+  }
+}
+
+// The steps of one matrix.  LDS: S, T, Q as [SP][SP + 4] doubles (the 4: 8 rows x 4 columns of a fragment read share no bank)
+constexpr int STEP_THREADS = 512;
+template <int SP>
+struct StepMatrices {
+  static constexpr int P = SP + 4, NI = SP / 16, NB = NI * (NI + 1) / 2, WAVES = STEP_THREADS / 64;
+  // block q of the product of two symmetric matrices that commute
+  static __device__ __forceinline__ f64x4_t block(const double* x, const double* y, int q) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
+    int bi, bj;
+    block_at(q, bi, bj);
+    const double* px = x + (16 * bi + l16) * P + lg;
+    const double* py = y + (16 * bj + l16) * P + lg;
+    f64x4_t d = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int k = 0; k < SP; k += 4) d = __builtin_amdgcn_mfma_f64_16x16x4f64(px[k], py[k], d, 0, 0, 0);
+    return d;
+  }
+  // both triangles
+  static __device__ __forceinline__ void put(double* m, int q, const f64x4_t& d) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
+    int bi, bj;
+    block_at(q, bi, bj);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int r = 16 * bi + 4 * v + lg, c = 16 * bj + l16;
+      m[r * P + c] = d[v];
+      if (bi != bj) m[c * P + r] = d[v];
+    }
+  }
+};
+
+// Q (times scale) in fp32, [SP][SP] and behind it what U is normalised by
+template <int SP>
+__global__ __launch_bounds__(STEP_THREADS) void narrow_steps_kernel(OrthPrepArgs a, int nparts, float* q_out) {
+  typedef StepMatrices<SP> M;
+  constexpr int P = M::P, NB = M::NB, WAVES = M::WAVES, MINE = (NB + WAVES - 1) / WAVES, MINE2 = (2 * NB + WAVES - 1) / WAVES;
+  extern __shared__ __attribute__((aligned(16))) double mem[];
+  double *S = mem, *T = mem + SP * P, *Q = mem + 2 * SP * P;
+  const int b = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
+  const double* parts = a.parts + (int64_t)b * nparts * (NB * 256);
+  for (int e = tid; e < NB * 256; e += STEP_THREADS) {
+    double s = 0.0;
+#pragma unroll 8
+    for (int p = 0; p < nparts; ++p) s += parts[(int64_t)p * (NB * 256) + e];
+    int bi, bj;
+    block_at(e >> 8, bi, bj);
+    const int r = 16 * bi + ((e >> 4) & 15), c = 16 * bj + (e & 15);
+    S[r * P + c] = s;
+    if (bi != bj) S[c * P + r] = s;
+  }
+  for (int e = tid; e < SP * SP; e += STEP_THREADS) Q[e / SP * P + e % SP] = e / SP == e % SP ? 1.0 : 0.0;
+  __syncthreads();
+  double trace = 0.0;
+  for (int i = 0; i < SP; ++i) trace += S[i * P + i];
+  const double f = 1.0 / (sqrt(trace) + (double)a.p.eps);
+  __syncthreads();
+  for (int e = tid; e < SP * SP; e += STEP_THREADS) S[e / SP * P + e % SP] *= f * f;
+  __syncthreads();
+  const double ca = a.p.a, cb = a.p.b, cc = a.p.c;
+  for (int t = 0; t < a.p.steps; ++t) {
+    f64x4_t d[MINE2];
+#pragma unroll
+    for (int n = 0; n < MINE; ++n) {
+      const int q = wave + n * WAVES;
+      if (q >= NB) break;
+      d[n] = M::block(S, S, q);
+      const int lane = tid & 63, l16 = lane & 15, lg = lane >> 4;
+      int bi, bj;
+      block_at(q, bi, bj);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int r = 16 * bi + 4 * v + lg, c = 16 * bj + l16;
+        d[n][v] = fma(cc, d[n][v], cb * S[r * P + c]) + (r == c ? ca : 0.0);
+      }
+      M::put(T, q, d[n]);
+    }
+    __syncthreads();
+    const bool last = t + 1 == a.p.steps;
+    // T Q, and S T into the place of S
+    const int blocks = last ? NB : 2 * NB;
+#pragma unroll
+    for (int n = 0; n < MINE2; ++n) {
+      const int q = wave + n * WAVES;
+      if (q >= blocks) break;
+      d[n] = q < NB ? M::block(T, Q, q) : M::block(S, T, q - NB);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < MINE2; ++n) {
+      const int q = wave + n * WAVES;
+      if (q >= blocks) break;
+      M::put(q < NB ? Q : S, q < NB ? q : q - NB, d[n]);
+    }
+    __syncthreads();
+    if (last) break;
+#pragma unroll
+    for (int n = 0; n < MINE; ++n) {
+      const int q = wave + n * WAVES;
+      if (q < NB) d[n] = M::block(S, T, q);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < MINE; ++n) {
+      const int q = wave + n * WAVES;
+      if (q < NB) M::put(S, q, d[n]);
+    }
+    __syncthreads();
+  }
+  float* out = q_out + (int64_t)b * (SP * SP + 4);
+  for (int e = tid; e < SP * SP; e += STEP_THREADS) out[e] = (float)((double)a.p.scale * Q[e / SP * P + e % SP]);
+  if (tid == 0) out[SP * SP] = (float)f;
+}
+
+// O = Q (f U): a wavefront takes 16 of a tile's 64 elements of the long side
+template <int SP, bool BF16G, bool VEC>
+__global__ __launch_bounds__(256) void narrow_apply_kernel(OrthPrepArgs a, int tiles, const float* q_in, void* out, bool vec_out) {
+  constexpr int NI = SP / 16, QP = SP + 1;
+  __shared__ float U[SP * UP];
+  __shared__ float Q[SP * QP];
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lg = lane >> 4;
+  const float* q = q_in + (int64_t)b * (SP * SP + 4);
+  for (int e = tid; e < SP * SP; e += 256) Q[e / SP * QP + e % SP] = q[e];
+  const float f = q[SP * SP];
+  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+    __syncthreads();
+    load_tile<SP, BF16G, VEC, false>(a, b, t, f, U);
+    __syncthreads();
+    f32x4_t acc[NI];
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < SP; k += 4) {
+      const float x = U[(k + lg) * UP + wave * 16 + l16];
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, Q[(k + lg) * QP + 16 * j + l16], acc[j], 0, 0, 0);
+    }
+    const int64_t il = (int64_t)t * LT + wave * 16 + 4 * lg;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int is = 16 * j + l16;
+      if (is >= a.s) continue;
+      const int64_t at = (int64_t)b * a.p.stride_o + (a.tall ? il * a.p.ld_o + is : is * a.p.ld_o + il);
+      if (vec_out && !a.tall && il + 4 <= a.l) {
+        if (a.p.out_dtype == GECC_F32) *reinterpret_cast<f32x4_t*>(static_cast<float*>(out) + at) = acc[j];
+        else *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(out) + at) =
+                 u32x2_t{(unsigned)to_bf16(acc[j][0]) | ((unsigned)to_bf16(acc[j][1]) << 16), (unsigned)to_bf16(acc[j][2]) | ((unsigned)to_bf16(acc[j][3]) << 16)};
+        continue;
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        if (il + v >= a.l) continue;
+        const int64_t to = at + v * (a.tall ? a.p.ld_o : 1);
+        if (a.p.out_dtype == GECC_F32) static_cast<float*>(out)[to] = acc[j][v];
+        else static_cast<uint16_t*>(out)[to] = to_bf16(acc[j][v]);
+      }
+    }
+  }
+}
+
+int side(int s) { return s <= 16 ? 16 : s <= 32 ? 32 : 64; }
+int block_doubles(int sp) { return sp / 16 * (sp / 16 + 1) / 2 * 256; }
+
+template <int SP, bool BF16G, bool VEC>
+hipError_t narrow(const OrthPrepArgs& a, void* out, float* q, bool vec_out, hipStream_t st) {
+  const int tiles = (a.l + LT - 1) / LT;
+  hipLaunchKernelGGL((narrow_gram_kernel<SP, BF16G, VEC>), dim3(a.nparts, a.p.batch), dim3(256), 0, st, a, tiles);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  constexpr int lds = 3 * SP * (SP + 4) * 8;
+  if (lds > 65536) {
+    static LdsLimit limit;
+    e = limit.raise(reinterpret_cast<const void*>(narrow_steps_kernel<SP>), lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((narrow_steps_kernel<SP>), dim3(a.p.batch), dim3(STEP_THREADS), lds, st, a, a.nparts, q);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int most = a.p.batch >= 1024 ? 1 : 1024 / a.p.batch;
+  hipLaunchKernelGGL((narrow_apply_kernel<SP, BF16G, VEC>), dim3(tiles < most ? tiles : most, a.p.batch), dim3(256), 0, st, a, tiles, q, out, vec_out);
+  return hipGetLastError();
+}
+template <int SP>
+hipError_t narrow(const OrthPrepArgs& a, void* out, float* q, bool vec_out, hipStream_t st) {
+  const bool vec = vectors_ok(a);
+  if (a.p.dtype == GECC_BF16) return vec ? narrow<SP, true, true>(a, out, q, vec_out, st) : narrow<SP, true, false>(a, out, q, vec_out, st);
+  return vec ? narrow<SP, false, true>(a, out, q, vec_out, st) : narrow<SP, false, false>(a, out, q, vec_out, st);
+}
+
+}  // namespace
+
+// up to 32 ranges of the long side for one matrix (their sums are read by one workgroup), fewer for many
+int orth_narrow_parts(int l, int batch) {
+  const int tiles = (l + LT - 1) / LT, most = batch >= 256 ? 1 : batch >= 8 ? 256 / batch : 32;
+  return tiles < most ? tiles : most;
+}
+size_t orth_narrow_part_bytes(int s, int nparts, int batch) { return (size_t)batch * nparts * block_doubles(side(s)) * sizeof(double); }
+size_t orth_narrow_q_bytes(int s, int batch) { return (size_t)batch * (side(s) * side(s) + 4) * sizeof(float); }
+
+hipError_t launch_orth_narrow(const OrthPrepArgs& a, void* out, float* q, hipStream_t st) {
+  if (a.s > ORTH_NARROW) return hipErrorInvalidValue;
+  const bool vec_out = orth_vec_out(a, out);
+  switch (side(a.s)) {
+    case 16: return narrow<16>(a, out, q, vec_out, st);
+    case 32: return narrow<32>(a, out, q, vec_out, st);
+    default: return narrow<64>(a, out, q, vec_out, st);
+  }
+}
+
+}  // namespace gecc

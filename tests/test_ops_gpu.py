@@ -274,7 +274,7 @@ def _orth_check(o, want, out):
 
 @pytest.mark.parametrize("kind", ["noise", "spiked", "rank"])
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 100), (100, 1), (16, 16), (33, 65), (64, 64), (65, 64), (128, 128), (127, 129), (129, 130), (200, 776), (776, 200),
-                                       (300, 301), (512, 512), (900, 130)])
+                                       (300, 301), (512, 512), (900, 130), (1, 300), (5, 700), (16, 257), (17, 1000), (40, 2049), (64, 600), (1000, 33), (700, 64)])
 def test_orthogonalised(rows, cols, kind):
     rng = _rng(rows, cols, 4)
     g, t = _store(1e-3 * _gradient(rng, rows, cols, kind), "bf16")
@@ -285,7 +285,7 @@ def test_orthogonalised(rows, cols, kind):
 
 @pytest.mark.parametrize("nesterov", [True, False])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,cols", [(40, 100), (257, 300), (600, 200)])
+@pytest.mark.parametrize("rows,cols", [(40, 100), (257, 300), (600, 200), (30, 1000), (555, 60)])
 def test_momentum(rows, cols, dtype, nesterov):
     rng = _rng(rows, cols, 5)
     m = torch.zeros(rows, cols, device=DEV)
@@ -298,7 +298,7 @@ def test_momentum(rows, cols, dtype, nesterov):
         assert np.abs(m.double().cpu().numpy() - ref).max() <= 3 * 2.0 ** -24 * np.abs(ref).max()     # a rounding a step
 
 
-@pytest.mark.parametrize("batch,rows,cols", [(3, 40, 100), (5, 128, 128), (7, 200, 70), (2, 600, 513), (40, 64, 64)])
+@pytest.mark.parametrize("batch,rows,cols", [(3, 40, 100), (5, 128, 128), (7, 200, 70), (2, 600, 513), (40, 64, 64), (3, 20, 700), (9, 500, 64)])
 def test_batches_are_their_items(batch, rows, cols):
     rng = _rng(batch, rows, cols, 6)
     g = _store(_gradient(rng, batch * rows, cols, "spiked").reshape(batch, rows, cols), "f32")[1]
@@ -314,7 +314,7 @@ def test_batches_are_their_items(batch, rows, cols):
 
 
 @pytest.mark.parametrize("steps", [0, 1, 2, 16])
-@pytest.mark.parametrize("rows,cols", [(50, 90), (300, 140)])
+@pytest.mark.parametrize("rows,cols", [(50, 90), (300, 140), (40, 400)])
 def test_numbers_of_steps(rows, cols, steps):
     """Coefficients whose polynomial has 1 as a fixed point of slope 0, so that more steps do not add error: 15 s / 8 ..."""
     rng = _rng(rows, cols, steps)
@@ -344,7 +344,7 @@ def test_nothing_to_orthogonalise_and_no_number():
 
 def test_strided_gradients_momenta_and_outputs():
     rng = _rng(12)
-    for rows, cols in ((70, 131), (300, 90)):
+    for rows, cols in ((70, 131), (300, 90), (20, 501), (333, 50)):
         g = _store(_gradient(rng, rows, cols, "spiked"), "bf16")[1]
         big_g = torch.full((rows, cols + 13), float("nan"), device=DEV, dtype=torch.bfloat16)
         big_m = torch.full((rows, cols + 7), 5.0, device=DEV)
