@@ -1,0 +1,103 @@
+"""A small training loop on one GPU that uses the operators of ops.py together, next to the protected product:
+
+    python -m paper_2508_04355_amd.train_layer [--steps 60] [--tokens 512] [--width 256] [--hidden 512] [--protect]
+
+Two linear layers with a ReLU between them learn a fixed random network of the same shape.  Each step quantises weights and
+activations to microscaled 4 bits (both ways in one pass, for the forward product and for the gradients), takes the three
+products of each layer on them, and applies the orthogonalised update to fp32 weights.  With --protect the weight gradients come
+from the protected bf16 product instead, with its report of errors found.  At the end one token goes through the layers from
+their packed weights, as a serving step does."""
+import argparse
+
+import torch
+
+from . import gecc, ops
+
+
+class Layer:
+    """y = x w^T with quantised operands; keeps what its backward pass needs."""
+
+    def __init__(self, k, m, seed, device, lr, protect):
+        g = torch.Generator(device=device).manual_seed(seed)
+        self.w = torch.randn(m, k, device=device, generator=g) * k ** -0.5
+        self.momentum = torch.zeros_like(self.w)
+        self.lr, self.protect = lr, protect
+        self.status = gecc.CLEAN
+
+    def forward(self, x):
+        w, self.wt = ops.mx4_quantize(self.w, both=True)
+        q, self.xt = ops.mx4_quantize(x, both=True)
+        self.x = x
+        return ops.mx4_gemm(q, w, dtype=torch.float32)
+
+    def backward(self, dy):
+        if not self.protect:
+            return ops.mx4_linear_backward(dy, self.wt, self.xt)
+        dx, _ = ops.mx4_linear_backward(dy, self.wt, None)
+        return dx, self.protected_gradient(dy)
+
+    def protected_gradient(self, dy):
+        """dy^T x in bf16 through the grid code: A is stored k x n, as dy is."""
+        (n, m), k = dy.shape, self.x.shape[1]
+        # (the noise model takes the terms of a sum to be independent; those of a gradient point the same way, so that their sums,
+        # and the roundings of these, grow with the number of tokens instead of its root)
+        rms = [float(t.square().mean().sqrt()) for t in (dy, self.x)]
+        tau = gecc.noise_thresholds(m, n, k, *rms, safety=16.0 * n ** 0.5)
+        ctx = gecc.Context(m, n, k, gecc.BF16, tau, trans_a=1, device=str(dy.device))
+        parities, report, dw = ctx.alloc_parities(), ctx.alloc_report(), ctx.alloc_c()
+        ctx.protected_gemm(dy.bfloat16().contiguous(), self.x.bfloat16().contiguous(), dw, *parities, report)
+        self.status = max(self.status, ctx.report_to_host(report)[0].status)
+        return dw[0]
+
+    def update(self, dw):
+        m, k = self.w.shape
+        self.w -= self.lr * ops.orthogonalize(dw, momentum=self.momentum, scale=max(1.0, m / k) ** 0.5, dtype=torch.float32)
+
+
+def train(steps=60, tokens=512, width=256, hidden=512, lr=0.02, protect=False, seed=1, device="cuda:0"):
+    """(losses by step, worst status of the protected products, the layers)"""
+    g = torch.Generator(device=device).manual_seed(seed)
+    x = torch.randn(tokens, width, device=device, generator=g)
+    teacher = [torch.randn(hidden, width, device=device, generator=g) * width ** -0.5,
+               torch.randn(width, hidden, device=device, generator=g) * hidden ** -0.5]
+    target = torch.relu(x @ teacher[0].t()) @ teacher[1].t()
+    layers = [Layer(width, hidden, seed + 1, device, lr, protect), Layer(hidden, width, seed + 2, device, lr, protect)]
+    losses = []
+    for step in range(steps):
+        h = layers[0].forward(x)
+        a = torch.relu(h)
+        y = layers[1].forward(a)
+        err = y - target
+        losses.append(float(err.square().mean()))
+        da, dw1 = layers[1].backward(err / tokens)
+        _, dw0 = layers[0].backward(da * (h > 0))
+        scale = 1.0 - step / steps
+        for layer, dw in zip(layers, (dw0, dw1)):
+            layer.lr = lr * scale
+            layer.update(dw)
+    return losses, max(layer.status for layer in layers), layers
+
+
+def serve(layers, token):
+    """One token (1 x width) through the packed weights."""
+    w0, w1 = (ops.mx4_quantize(layer.w) for layer in layers)
+    return ops.mx4_linear(torch.relu(ops.mx4_linear(token, w0)), w1)
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    for name, value in (("steps", 60), ("tokens", 512), ("width", 256), ("hidden", 512)):
+        ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--protect", action="store_true")
+    a = ap.parse_args()
+    losses, status, layers = train(a.steps, a.tokens, a.width, a.hidden, protect=a.protect)
+    for i in sorted({0, a.steps // 4, a.steps // 2, a.steps - 1}):
+        print("step %3d  loss %.5f" % (i, losses[i]))
+    if a.protect:
+        print("protected weight gradients: worst status %d (%d is clean)" % (status, gecc.CLEAN))
+    y = serve(layers, torch.randn(1, a.width, device="cuda:0"))
+    print("one token: %d values, finite: %s" % (y.numel(), bool(torch.isfinite(y).all())))
+
+
+if __name__ == "__main__":
+    main()

@@ -421,3 +421,22 @@ def test_in_a_graph():
         for a, b in zip(want, got):
             assert torch.equal(a, b), i
         assert torch.equal(m, m_ref)
+
+
+# ---- together ------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("protect", [False, True])
+def test_a_layer_learns(protect):
+    """The example: the loss at least halves (a layer that did not learn would keep it), the protected gradients report no
+    errors, and a token served from packed weights gets what the batch gets."""
+    from paper_2508_04355_amd import train_layer
+    losses, status, layers = train_layer.train(steps=60, tokens=256, width=128, hidden=200, protect=protect)
+    assert np.isfinite(losses).all() and losses[-1] < losses[0] / 2
+    assert status == gecc.CLEAN
+    x = torch.randn(70, 128, device=DEV)
+    h = torch.relu(ops.mx4_gemm(ops.mx4_quantize(x), ops.mx4_quantize(layers[0].w)))
+    y = ops.mx4_gemm(ops.mx4_quantize(h), ops.mx4_quantize(layers[1].w))
+    for i in (0, 33, 69):
+        # (the fp32 sums of one row may be formed in another order: half an ulp at their size, then quantised again)
+        one = train_layer.serve(layers, x[i:i + 1])
+        assert float((one - y[i]).norm() / y[i].norm()) < 0.02
