@@ -81,22 +81,30 @@ __global__ __launch_bounds__(256) void mx4_cols_kernel(MxQuantArgs a, int col_ti
   constexpr int TR = 128, TC = F32 ? 64 : 128, LANES = TC / 8;      // lanes that hold a row
   __shared__ __attribute__((aligned(16))) char tile[TR * 256];
   const int tid = threadIdx.x;
-  const int c0 = (blockIdx.x % col_tiles) * TC;
-  const int64_t r0 = (int64_t)(blockIdx.x / col_tiles) * TR;
+  // (workgroups go round the XCDs: each of them gets neighbouring tiles, whose halves of a line then meet in its L2)
+  int pid = blockIdx.x;
+  {
+    const int per = gridDim.x / 8, rem = gridDim.x % 8, x = pid & 7;
+    pid = x * per + min(x, rem) + (pid >> 3);
+  }
+  const int c0 = (pid % col_tiles) * TC;
+  const int64_t r0 = (int64_t)(pid / col_tiles) * TR;
   const int64_t pitch = mx_pad(a.cols) / 2, t_pitch = mx_pad(a.rows) / 2;
   const int c = c0 + (tid % LANES) * 8;
   constexpr int STEP = 256 / LANES, ITER = TR / STEP;
   const int64_t rows16 = (a.rows + 15) / 16 * 16;
+  // (all of a thread's loads on their way together where they are vectors, else two at a time)
+  constexpr int GROUP = VEC ? ITER : 2;
 #pragma unroll 1
-  for (int it0 = 0; it0 < ITER; it0 += 4) {
-    float v[4][8];
+  for (int it0 = 0; it0 < ITER; it0 += GROUP) {
+    float v[GROUP][8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < GROUP; ++q) {
       const int64_t row = r0 + (it0 + q) * STEP + tid / LANES;
       load8<F32, VEC>(a.X, row * a.ld + c, c, a.cols, row < a.rows, v[q]);
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < GROUP; ++q) {
       const int rr = (it0 + q) * STEP + tid / LANES;
       const int64_t row = r0 + rr;
       if (F32) {
@@ -202,7 +210,8 @@ __global__ __launch_bounds__(256) void mx4_values_kernel(MxDequantArgs a, int un
 constexpr int FEW_WAVES = 8;
 constexpr int FEW_RAW_BYTES = 32768;      // packed X that a workgroup keeps
 
-template <int NG, bool RAW, bool F32X>
+// FEW_UNITS: units of a wavefront whose weights are on their way together
+template <int NG, int FEW_UNITS, bool RAW, bool F32X>
 __global__ __launch_bounds__(FEW_WAVES * 64) void mx4_few_kernel(MxFewArgs a, int units, bool vec_x, bool vec_y) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -212,6 +221,24 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void mx4_few_kernel(MxFewArgs a, in
   const int w0 = blockIdx.x * 16;
   const uint8_t* wrow = a.w_data + (int64_t)min(w0 + l16, a.m - 1) * pitch + g * 16;
   const uint8_t* wsc = a.w_scales + ((int64_t)blockIdx.x * units) * 256 + l16 * 16 + g * 4;
+  // This wavefront's part of the weight, up to four of its units (4 KiB each) at a time, asked for before anything else: memory is
+  // what the kernel waits for
+  u32x4_t w[FEW_UNITS][4];
+  int ws[FEW_UNITS];
+  auto load_weight = [&](int u0) {
+#pragma unroll
+    for (int h = 0; h < FEW_UNITS; ++h) {
+      const int u = u0 + h * FEW_WAVES, left = steps - 4 * u;         // 4 or more, or 2 in a last half unit
+      ws[h] = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[h][j] = u32x4_t{0, 0, 0, 0};
+        if (j < left) w[h][j] = *reinterpret_cast<const u32x4_t*>(wrow + (int64_t)(4 * u + j) * 64);
+      }
+      if (left > 0) ws[h] = *reinterpret_cast<const int*>(wsc + (int64_t)u * 256);
+    }
+  };
+  load_weight(wave);
   char* xs = smem + FEW_WAVES * NG * 1024;                   // RAW: data [steps * n * 64], then scales [units * n * 16]
   char* xsc = xs + (size_t)steps * a.n * 64;
   if (RAW) {
@@ -238,41 +265,42 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void mx4_few_kernel(MxFewArgs a, in
   f32x4_t acc[NG];
 #pragma unroll
   for (int q = 0; q < NG; ++q) acc[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int u = wave; u < units; u += FEW_WAVES) {
-    u32x4_t w[4], x[NG][4];
-    int ws, sx[NG];
-    const int left = steps - 4 * u;          // 4, or 2 in a last half unit
+  for (int u0 = wave; u0 < units; u0 += FEW_UNITS * FEW_WAVES) {
+    if (u0 != wave) load_weight(u0);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = j < left ? *reinterpret_cast<const u32x4_t*>(wrow + (int64_t)(4 * u + j) * 64) : u32x4_t{0, 0, 0, 0};
-    ws = *reinterpret_cast<const int*>(wsc + (int64_t)u * 256);
+    for (int h = 0; h < FEW_UNITS; ++h) {
+      const int u = u0 + h * FEW_WAVES, left = steps - 4 * u;
+      if (left <= 0) break;
+      u32x4_t x[NG][4];
+      int sx[NG];
 #pragma unroll
-    for (int q = 0; q < NG; ++q) {
-      const int row = q * 16 + l16;
-      const bool ok = row < a.n;
-      sx[q] = 0;
-      if (ok) sx[q] = RAW ? *reinterpret_cast<const int*>(xsc + ((u * a.n + row) * 4 + g) * 4)
-                          : *reinterpret_cast<const int*>(a.x_scales + ((int64_t)q * units + u) * 256 + l16 * 16 + g * 4);
+      for (int q = 0; q < NG; ++q) {
+        const int row = q * 16 + l16;
+        const bool ok = row < a.n;
+        sx[q] = 0;
+        if (ok) sx[q] = RAW ? *reinterpret_cast<const int*>(xsc + ((u * a.n + row) * 4 + g) * 4)
+                            : *reinterpret_cast<const int*>(a.x_scales + ((int64_t)q * units + u) * 256 + l16 * 16 + g * 4);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[q][j] = u32x4_t{0, 0, 0, 0};
-        if (ok && j < left)
-          x[q][j] = RAW ? *reinterpret_cast<const u32x4_t*>(xs + (((4 * u + j) * a.n + row) * 4 + g) * 16)
-                        : *reinterpret_cast<const u32x4_t*>(a.x_data + (int64_t)row * pitch + (4 * u + j) * 64 + g * 16);
+        for (int j = 0; j < 4; ++j) {
+          x[q][j] = u32x4_t{0, 0, 0, 0};
+          if (ok && j < left)
+            x[q][j] = RAW ? *reinterpret_cast<const u32x4_t*>(xs + (((4 * u + j) * a.n + row) * 4 + g) * 16)
+                          : *reinterpret_cast<const u32x4_t*>(a.x_data + (int64_t)row * pitch + (4 * u + j) * 64 + g * 16);
+        }
       }
-    }
 #pragma unroll
-    for (int q = 0; q < NG; ++q) {
+      for (int q = 0; q < NG; ++q) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (j >= left) break;                // (there are no scales either)
-        const i32x8_t fa = {(int)w[j][0], (int)w[j][1], (int)w[j][2], (int)w[j][3], 0, 0, 0, 0};
-        const i32x8_t fb = {(int)x[q][j][0], (int)x[q][j][1], (int)x[q][j][2], (int)x[q][j][3], 0, 0, 0, 0};
-        // (the byte of the scale registers is a constant of the instruction)
-        if (j == 0) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 0, ws, 0, sx[q]);
-        if (j == 1) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 1, ws, 1, sx[q]);
-        if (j == 2) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 2, ws, 2, sx[q]);
-        if (j == 3) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 3, ws, 3, sx[q]);
+        for (int j = 0; j < 4; ++j) {
+          if (j >= left) break;                // (there are no scales either)
+          const i32x8_t fa = {(int)w[h][j][0], (int)w[h][j][1], (int)w[h][j][2], (int)w[h][j][3], 0, 0, 0, 0};
+          const i32x8_t fb = {(int)x[q][j][0], (int)x[q][j][1], (int)x[q][j][2], (int)x[q][j][3], 0, 0, 0, 0};
+          // (the byte of the scale registers is a constant of the instruction)
+          if (j == 0) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 0, ws[h], 0, sx[q]);
+          if (j == 1) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 1, ws[h], 1, sx[q]);
+          if (j == 2) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 2, ws[h], 2, sx[q]);
+          if (j == 3) acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, acc[q], 4, 4, 3, ws[h], 3, sx[q]);
+        }
       }
     }
   }
@@ -307,7 +335,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void mx4_few_kernel(MxFewArgs a, in
   }
 }
 
-template <int NG>
+template <int NG, int FU>
 hipError_t few(const MxFewArgs& a, int units, hipStream_t st) {
   const int64_t es = a.x_dtype == GECC_F32 ? 4 : 2, ey = a.y_dtype == GECC_F32 ? 4 : 2;
   const bool vec_x = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * es % 16 == 0;
@@ -316,12 +344,18 @@ hipError_t few(const MxFewArgs& a, int units, hipStream_t st) {
   size_t lds = FEW_WAVES * NG * 1024;
   if (a.x) {
     lds += (size_t)a.n * mx_pad(a.k) / 2 + (size_t)a.n * units * 16;
-    if (a.x_dtype == GECC_F32) hipLaunchKernelGGL((mx4_few_kernel<NG, true, true>), grid, block, lds, st, a, units, vec_x, vec_y);
-    else hipLaunchKernelGGL((mx4_few_kernel<NG, true, false>), grid, block, lds, st, a, units, vec_x, vec_y);
+    if (a.x_dtype == GECC_F32) hipLaunchKernelGGL((mx4_few_kernel<NG, FU, true, true>), grid, block, lds, st, a, units, vec_x, vec_y);
+    else hipLaunchKernelGGL((mx4_few_kernel<NG, FU, true, false>), grid, block, lds, st, a, units, vec_x, vec_y);
   } else {
-    hipLaunchKernelGGL((mx4_few_kernel<NG, false, false>), grid, block, lds, st, a, units, vec_x, vec_y);
+    hipLaunchKernelGGL((mx4_few_kernel<NG, FU, false, false>), grid, block, lds, st, a, units, vec_x, vec_y);
   }
   return hipGetLastError();
+}
+
+template <int NG>
+hipError_t few(const MxFewArgs& a, int units, hipStream_t st) {
+  // (short rows: fewer registers, more workgroups a compute unit)
+  return units <= FEW_WAVES ? few<NG, 1>(a, units, st) : units <= 2 * FEW_WAVES ? few<NG, 2>(a, units, st) : few<NG, 4>(a, units, st);
 }
 
 template <bool F32, bool VEC>
