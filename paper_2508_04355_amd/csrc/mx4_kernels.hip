@@ -163,8 +163,8 @@ __global__ __launch_bounds__(256) void mx4_cols_kernel(MxQuantArgs a, int col_ti
   const int c = c0 + (tid % LANES) * 8;
   constexpr int STEP = 256 / LANES, ITER = TR / STEP;
   const int64_t rows16 = (a.rows + 15) / 16 * 16;
-  // (all of a thread's loads on their way together where they are vectors, else two at a time)
-  constexpr int GROUP = VEC ? ITER : 2;
+  // all of a thread's loads on their way together, four at a time where they are single values
+  constexpr int GROUP = VEC ? ITER : 4;
 #pragma unroll 1
   for (int it0 = 0; it0 < ITER; it0 += GROUP) {
     Eight<F32> v[GROUP];

@@ -15,8 +15,10 @@ __global__ __launch_bounds__(THREADS, 1) void tile256_kernel(TileArgs a, bool ve
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wr = wave >> 1, wc = wave & 1;
-  const int b = blockIdx.y;
-  int tile = blockIdx.x, range = 0;
+  unsigned group = blockIdx.x, item = 0;
+  if (gridDim.y > 1) batch_place(gridDim.x, gridDim.y, blockIdx.x + gridDim.x * blockIdx.y, group, item);
+  const int b = item;
+  int tile = group, range = 0;
   const bool shared = tile >= a.whole;
   if (shared) {
     const unsigned y = tile - a.whole;
@@ -25,6 +27,7 @@ __global__ __launch_bounds__(THREADS, 1) void tile256_kernel(TileArgs a, bool ve
   }
   int tm, tn;
   if (a.symmetric) triangle(tile, tm, tn);
+  else if (gridDim.y > 1) { const int ntm = (a.m_rows + BM - 1) / BM; tm = tile % ntm; tn = tile / ntm; }
   else tile_of(tile, (a.m_rows + BM - 1) / BM, (a.n_rows + BN - 1) / BN, 0, 0, tm, tn);
   const int r0 = tm * BM, c0 = tn * BN;
   // stages of 128 bytes of k (a pair of k-tiles), shared out in twos: four k-tiles have their scales in one word
@@ -53,7 +56,7 @@ __global__ __launch_bounds__(THREADS, 1) void tile256_kernel(TileArgs a, bool ve
   multiply_256<KIND == KIND_MX4 ? T256_MX4 : T256_F16, KCA, true, true>(acc, oa, ob, sc, smem, KT, __builtin_amdgcn_readfirstlane(p0));
 
   if (shared) {               // in the order of the registers, as tile_finish_kernel takes them
-    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + ((int64_t)b * (gridDim.x - a.whole) + (blockIdx.x - a.whole)) * (BM * BN / 4) + wave * 4096 + lane;
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + ((int64_t)b * (gridDim.x - a.whole) + (group - a.whole)) * (BM * BN / 4) + wave * 4096 + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll

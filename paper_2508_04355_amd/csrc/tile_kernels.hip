@@ -129,14 +129,16 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int wr = wave >> 1, wc = wave & 1, l16 = lane & 15, g = lane >> 4;
-  const int b = blockIdx.z;
+  unsigned group = blockIdx.x + gridDim.x * blockIdx.y, item = 0;
+  if (gridDim.z > 1) batch_place(gridDim.x * gridDim.y, gridDim.z, group + gridDim.x * gridDim.y * blockIdx.z, group, item);
+  const int b = item, tile = group % gridDim.x, range = group / gridDim.x;
   int tm, tn;
-  tile_at<T>(a, blockIdx.x, tm, tn);
+  tile_at<T>(a, tile, tm, tn);
   const int r0 = tm * T, c0 = tn * T;
   // this workgroup's stages: a range of whole pairs (a scale tile is two stages long)
   const int pairs = (a.stages + 1) / 2;
-  const int first = (int)((int64_t)pairs * blockIdx.y / a.split) * 2;
-  const int last = min((int)((int64_t)pairs * (blockIdx.y + 1) / a.split) * 2, a.stages);
+  const int first = (int)((unsigned)pairs * range / (unsigned)a.split) * 2;
+  const int last = min((int)((unsigned)pairs * (range + 1) / (unsigned)a.split) * 2, a.stages);
   const int count = last - first;
 
   TileOperand<KCA, T> oa;
@@ -269,7 +271,7 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
 
   if (a.split > 1) {
     // [batch][tile][range][fragment pair][lane] in the order of the registers; tile_finish_kernel adds the ranges up
-    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + (((int64_t)b * gridDim.x + blockIdx.x) * a.split + blockIdx.y) * (T * T / 4) + wave * (F * F * 64) + lane;
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + (((int64_t)b * gridDim.x + tile) * a.split + range) * (T * T / 4) + wave * (F * F * 64) + lane;
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
@@ -277,7 +279,6 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
     return;
   }
   __syncthreads();               // the stages are done with: their LDS holds rows of the result now
-  static_assert(4 * store_floats<F>() * 4 <= RING * SLOT, "room for the epilogue");
   store_tile<EPI, F, F>(a, b, acc, reinterpret_cast<float*>(smem) + wave * store_floats<F>(), r0 + wr * (T / 2), c0 + wc * (T / 2), r0 + T, c0 + T,
                          a.symmetric && tm != tn, vec_out);
 }
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(256) void tile_finish_kernel(TileArgs a, bool vec_o
   const int t = piece / (4 * F * F), r = piece % (4 * F * F);   // t: of the `shared` tiles from number a.whole on
   if (t >= shared) return;
   int tm, tn;
-  if (T == 256 && !a.symmetric) tile_of(a.whole + t, (a.m_rows + T - 1) / T, (a.n_rows + T - 1) / T, 0, 0, tm, tn);
+  if (T == 256 && !a.symmetric && a.batch == 1) tile_of(a.whole + t, (a.m_rows + T - 1) / T, (a.n_rows + T - 1) / T, 0, 0, tm, tn);
   else tile_at<T>(a, a.whole + t, tm, tn);
   const int wave = r / (F * F), i = r % (F * F) / F, j = r % F;
   const f32x4_t* p = reinterpret_cast<const f32x4_t*>(a.part) + ((int64_t)b * shared + t) * a.split * (T * T / 4) + r * 64 + lane;
@@ -324,7 +325,8 @@ hipError_t launch(const TileArgs& a, hipStream_t st) {
   static_assert(RING % 2 == 0 && (RING & (RING - 1)) == 0, "slots of stages, and of their scales, by number");
   const int64_t tiles = tiles_of(a.m_rows, a.n_rows, T, a.symmetric);
   if (tiles > 0x7fffffff || a.batch > 65535) return hipErrorInvalidValue;
-  constexpr int lds = RING * 2 * T * 128 + (KIND == KIND_MX4 ? RING / 2 * 2 * T * 16 : 0);
+  constexpr int stages = RING * 2 * T * 128 + (KIND == KIND_MX4 ? RING / 2 * 2 * T * 16 : 0), rows = 4 * store_floats<T / 32>() * 4;
+  constexpr int lds = stages > rows ? stages : rows;            // (the epilogue has it afterwards)
   auto kern = tile_kernel<KIND, KCA, T, RING, EPI>;
   if (lds > 65536) {
     static LdsLimit limit;
@@ -405,10 +407,11 @@ hipError_t launch_any(const TileArgs& a, const TilePlan& plan, hipStream_t st) {
     const int64_t tiles = tiles_of(a.m_rows, a.n_rows, 256, a.symmetric);
     return e != hipSuccess || a.whole == tiles ? e : launch_finish<256, EPI>(a, tiles, st);
   }
-  // 64 KiB of LDS, two workgroups a compute unit; tiles of 128 that are no more than compute units have twice that
+  // 64 KiB of LDS, two workgroups a compute unit; tiles of 128 that are no more than compute units have twice that, more tiles
+  // of 64 than two a compute unit half (P X, 3001 x 801, 611 tiles: 15.2 -> 12.9 us, all of them at once)
   const int64_t groups = tiles_of(a.m_rows, a.n_rows, plan.tile, a.symmetric) * a.split * a.batch;
   if (plan.tile == 128) return groups <= 256 ? launch<KIND, KCA, 128, 4, EPI>(a, st) : launch<KIND, KCA, 128, 2, EPI>(a, st);
-  return launch<KIND, KCA, 64, 4, EPI>(a, st);
+  return groups <= 512 ? launch<KIND, KCA, 64, 4, EPI>(a, st) : launch<KIND, KCA, 64, 2, EPI>(a, st);
 }
 }  // namespace
 

@@ -45,5 +45,18 @@ __device__ __forceinline__ void triangle(int t, int& tm, int& tn) {
   tn = t - tm * (tm + 1) / 2;
 }
 
+// Batches of eight items or more: workgroup number `linear` of `groups` an item.  Workgroups go round the eight XCDs; all of an
+// item's go to one of them, in whose L2 they share its operands (256 x 512 x 512 in chunks of 64: 2025 -> 1739 us).
+__device__ __forceinline__ void batch_place(unsigned groups, unsigned batch, unsigned linear, unsigned& group, unsigned& item) {
+  if (linear < groups * (batch & ~7u)) {
+    const unsigned xcd = linear & 7, n = linear >> 3;
+    item = n / groups * 8 + xcd;
+    group = n % groups;
+  } else {
+    item = linear / groups;
+    group = linear % groups;
+  }
+}
+
 }  // namespace
 }  // namespace gecc
