@@ -204,6 +204,7 @@ __global__ __launch_bounds__(256) void mx4_cols_kernel(MxQuantArgs a, int col_ti
   }
   const int64_t row = r0 + rb * 32;
   const int64_t cols16 = ((int64_t)a.cols + 15) / 16 * 16;
+  __syncthreads();                                 // the tile has been read: its LDS takes the codes, 64 bytes a column
 #pragma unroll
   for (int h = 0; h < NC; ++h) {
     const unsigned s = scale_byte(top[h]);
@@ -223,9 +224,19 @@ __global__ __launch_bounds__(256) void mx4_cols_kernel(MxQuantArgs a, int col_ti
         out[p] = bf16_codes(q, s);
       }
     }
-    const int64_t cg = c0 + cc + h;
-    if (cg < a.cols && row / 2 < t_pitch) *reinterpret_cast<u32x4_t*>(a.t_data + cg * t_pitch + row / 2) = out;
+    const int col = cc + h;
+    *reinterpret_cast<u32x4_t*>(tile + col * 64 + ((rb ^ (col >> 1)) & 3) * 16) = out;
+    const int64_t cg = c0 + col;
     if (cg < cols16 && row < (int64_t)t_units * MX_UNIT) a.t_scales[scale_at(cg, row >> 5, t_units)] = (uint8_t)s;
+  }
+  __syncthreads();
+  // four lanes a column, 64 consecutive bytes
+#pragma unroll
+  for (int h = 0; h < TC * 4 / 256; ++h) {
+    const int q = h * 256 + tid, col = q >> 2, part = q & 3;
+    const int64_t cg = c0 + col, at = r0 / 2 + part * 16;
+    if (cg < a.cols && at < t_pitch)
+      *reinterpret_cast<u32x4_t*>(a.t_data + cg * t_pitch + at) = *reinterpret_cast<const u32x4_t*>(tile + col * 64 + ((part ^ (col >> 1)) & 3) * 16);
   }
 }
 

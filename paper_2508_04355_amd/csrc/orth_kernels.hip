@@ -452,7 +452,15 @@ hipError_t start(const OrthPrepArgs& a, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_orth_norm(const OrthPrepArgs& a, hipStream_t st) {
+hipError_t launch_orth_norm(const OrthPrepArgs& a0, hipStream_t st) {
+  OrthPrepArgs a = a0;
+  // Rows without gaps are one row: whatever their length, it is read in vectors (3001 x 801 fp32 with momentum: 18.5 -> 9.7 us)
+  const int64_t n = (int64_t)a.p.rows * a.p.cols;
+  if ((a.p.ld_g == a.p.cols || a.p.rows == 1) && (!a.M || a.p.ld_m == a.p.cols || a.p.rows == 1) && n < 0x7fffffff - 8) {
+    a.p.rows = 1;
+    a.p.cols = (int32_t)n;
+    a.p.ld_g = a.p.ld_m = 0;
+  }
   const dim3 grid(a.nparts, a.p.batch), block(256);
   const bool vec = vectors_ok(a);
   if (a.p.dtype == GECC_BF16) {

@@ -345,9 +345,11 @@ namespace {
 // Times (us) as fitted to measurements, both kinds of operand (a stage is 128 bytes of k a row, the same work for both): what
 // a round of workgroups takes beside its stages, and a stage with one workgroup a compute unit and with two.
 //                            measured / by this fit
-//   4-bit  512 x 4096 x 4096      tiles of 64 11.6 / 12   of 128 12.7 / 14   (128 workgroups)
-//   4-bit  2048 x 4096 x 4096     64 36.6 / 38   128 19.9 / 22   256 27.8 / 34
+//   4-bit  512 x 4096 x 4096      tiles of 64 12.0 / 12   of 128 12.7 / 14   (128 workgroups)
+//   4-bit  1024 x 4096 x 4096     64 17.3 / 18   128 16.7 / 14
+//   4-bit  2048 x 4096 x 4096     64 30.5 / 33   128 19.9 / 22   256 27.8 / 34
 //   4-bit  4096^3                 128 38.6 / 40   256 34.9 / 34
+//   fp16   P X, 801 x 3001        64 11.5 / 11   128 14.0 / 13
 //   fp16   X X^T, 2048 x 4096     64 41.9 / 44   128 35.4 / 38, in three ranges 34 / 39
 //   fp16   P X, 4096 x 14336      128 423 / 424   256 360 / 369
 double rounds_of(int64_t groups, int at_once) {
@@ -357,7 +359,8 @@ double rounds_of(int64_t groups, int at_once) {
 double tile_time(int tile, int64_t groups, double stages, bool mirrored) {
   if (tile == 256) return 3.0 + (double)((groups + 255) / 256) * (9.0 + 1.35 * stages);
   const double fixed = (tile == 128 ? 4.5 : 2.5) + (mirrored ? (tile == 128 ? 4.0 : 0.5) : 0.0);
-  if (groups <= 256) return 3.0 + fixed + stages * (tile == 128 ? 0.42 : 0.2);
+  if (tile == 64 && groups > 512) return 4.0 + (double)groups / 256.0 * (0.6 + 0.19 * stages);      // (four at once a compute unit)
+  if (groups <= 256) return 2.0 + fixed + stages * (tile == 128 ? 0.42 : 0.2);
   return 3.0 + rounds_of(groups, 512) * (fixed + stages * (tile == 128 ? 0.87 : 0.39));
 }
 double finish_time(size_t part_bytes) { return part_bytes ? 4.5 + 0.25e-6 * (double)part_bytes : 0.0; }
