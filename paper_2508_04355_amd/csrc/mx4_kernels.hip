@@ -284,7 +284,9 @@ __global__ __launch_bounds__(256) void mx4_values_kernel(MxDequantArgs a, int un
 // 16 NG rows of X as the second; its eight wavefronts share the units of 512 columns and add up through LDS, in order.
 // RAW: every workgroup quantises X itself, into LDS as [unit][step][group][lane] fragments.
 constexpr int FEW_WAVES = 8;
-constexpr int FEW_RAW_BYTES = 32768;      // packed X that a workgroup keeps
+// Packed X that a workgroup keeps. Twice as much saves a launch at 24 x 4096 to 2048 (12.8 us instead of 14.8), but the one
+// workgroup's quantisation is longer than a launch at more rows: 59 x 2000 to 533 took 23 us instead of 14.
+constexpr int FEW_RAW_BYTES = 32768;
 
 // FEW_UNITS: units of a wavefront whose weights are on their way together
 template <int NG, int FEW_UNITS, bool RAW, bool F32X>
@@ -322,18 +324,12 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void mx4_few_kernel(MxFewArgs a, in
     const int per_row = steps * 16, total = a.n * per_row;       // chunks of eight columns
     for (int o = tid; o < total; o += FEW_WAVES * 64) {     // (per_row is a multiple of 4: whole groups of lanes)
       const int row = o / per_row, c = (o - row * per_row) * 8;
-      float v[8];
-      if (vec_x) load8<F32X, true>(a.x, (int64_t)row * a.ldx + c, c, a.k, true, v);
-      else load8<F32X, false>(a.x, (int64_t)row * a.ldx + c, c, a.k, true, v);
-      unsigned m = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
-      const unsigned s = scale_byte(quad_max(m));
-      const float inv = inverse_scale(s);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = scaled(v[i], inv);
+      Eight<F32X> v;
+      if (vec_x) v.template load<true>(a.x, (int64_t)row * a.ldx + c, c, a.k, true);
+      else v.template load<false>(a.x, (int64_t)row * a.ldx + c, c, a.k, true);
+      const unsigned s = scale_byte(quad_max(v.amax()));
       const int step = c >> 7, blk = (c >> 5) & 3;
-      *reinterpret_cast<unsigned*>(xs + ((step * a.n + row) * 4 + blk) * 16 + ((c >> 3) & 3) * 4) = pack8(v);
+      *reinterpret_cast<unsigned*>(xs + ((step * a.n + row) * 4 + blk) * 16 + ((c >> 3) & 3) * 4) = v.codes(s);
       if ((o & 3) == 0) xsc[(((step >> 2) * a.n + row) * 4 + blk) * 4 + (step & 3)] = (char)s;
     }
     __syncthreads();
@@ -420,8 +416,9 @@ hipError_t few(const MxFewArgs& a, int units, hipStream_t st) {
   size_t lds = FEW_WAVES * NG * 1024;
   if (a.x) {
     lds += (size_t)a.n * mx_pad(a.k) / 2 + (size_t)a.n * units * 16;
-    if (a.x_dtype == GECC_F32) hipLaunchKernelGGL((mx4_few_kernel<NG, FU, true, true>), grid, block, lds, st, a, units, vec_x, vec_y);
-    else hipLaunchKernelGGL((mx4_few_kernel<NG, FU, true, false>), grid, block, lds, st, a, units, vec_x, vec_y);
+    const bool f32 = a.x_dtype == GECC_F32;
+    auto kern = f32 ? mx4_few_kernel<NG, FU, true, true> : mx4_few_kernel<NG, FU, true, false>;
+    hipLaunchKernelGGL(kern, grid, block, lds, st, a, units, vec_x, vec_y);
   } else {
     hipLaunchKernelGGL((mx4_few_kernel<NG, FU, false, false>), grid, block, lds, st, a, units, vec_x, vec_y);
   }

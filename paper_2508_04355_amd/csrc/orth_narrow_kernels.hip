@@ -21,7 +21,6 @@ typedef __attribute__((ext_vector_type(4))) double f64x4_t;
 constexpr int LT = 64;                       // elements of the long side of a tile
 constexpr int UP = LT + 1;
 
-__device__ __forceinline__ int block_count(int sp) { return sp / 16 * (sp / 16 + 1) / 2; }
 // block number q of the lower triangle
 __device__ __forceinline__ void block_at(int q, int& bi, int& bj) {
   bi = q < 1 ? 0 : q < 3 ? 1 : q < 6 ? 2 : 3;

@@ -12,7 +12,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import gecc
-from .gecc import BF16, F32, GeccError, _check, _ptr, _stream
+from .gecc import BF16, F32, GeccError, _check, _ptr, _raw_stream
 
 ORTH_MAX_STEPS = 16
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
@@ -56,13 +56,15 @@ def lib():
     return L
 
 
-def _matrix(t, what, dtypes=_DTYPES):
+def _matrix(t, what):
     """`t` as a device matrix whose rows are contiguous (a copy only where its last dimension is strided)."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _DTYPES and t.dim() == 2 and t.is_contiguous():
+        return t
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise GeccError("%s: a tensor on the GPU is wanted" % what)
     if t.dim() != 2:
         raise GeccError("%s: a matrix is wanted, got %d dimensions" % (what, t.dim()))
-    if t.dtype not in dtypes:
+    if t.dtype not in _DTYPES:
         raise GeccError("%s: %s is not supported (float32 and bfloat16 are)" % (what, t.dtype))
     return _rows(t)
 
@@ -93,6 +95,11 @@ def _bytes(name, *shape):
     return getattr(lib(), name)(*shape)
 
 
+@functools.lru_cache(maxsize=4096)
+def _mx4_bytes(rows, cols):
+    return lib().gecc_mx4_data_bytes(rows, cols), lib().gecc_mx4_scale_bytes(rows, cols)
+
+
 def _workspace(nbytes, device):
     """(tensor or None, its address, its size); torch's allocator hands out multiples of 512 bytes."""
     if not nbytes:
@@ -119,22 +126,27 @@ class Mx4:
         self._data, self._scales = data.data_ptr(), scales.data_ptr()
 
     @classmethod
-    def _new(cls, rows, cols, device):
-        """An empty one, both buffers in one allocation."""
-        q = cls.__new__(cls)
-        n = _bytes("gecc_mx4_data_bytes", rows, cols)
-        if n == 0:
+    def _new(cls, rows, cols, device, transposed=False):
+        """An empty one, and one of the transpose where asked for, all buffers in one allocation."""
+        sizes = _mx4_bytes(rows, cols) + (_mx4_bytes(cols, rows) if transposed else ())
+        if 0 in sizes:
             raise GeccError("mx4: a matrix of %d x %d" % (rows, cols))
-        both = torch.empty(n + _bytes("gecc_mx4_scale_bytes", rows, cols), dtype=torch.uint8, device=device)
-        q.rows, q.cols, q.device, q._kept = rows, cols, both.device, both
-        q._data = both.data_ptr()
-        q._scales = q._data + n         # (n is a multiple of 128)
+        memory = torch.empty(sum(sizes), dtype=torch.uint8, device=device)
+        q = cls._at(memory, memory.data_ptr(), rows, cols, device, sizes[0])
+        return (q, cls._at(memory, q._data + sizes[0] + sizes[1], cols, rows, device, sizes[2])) if transposed else q
+
+    @classmethod
+    def _at(cls, memory, address, rows, cols, device, data_bytes):
+        q = cls.__new__(cls)
+        q.rows, q.cols, q.device, q._kept = rows, cols, device, memory
+        q._data, q._scales = address, address + data_bytes         # (multiples of 128 and of 256 bytes)
         return q
 
     def _parts(self):
         if not isinstance(self._kept, tuple):
-            n = self._scales - self._data
-            self._kept = (self._kept[:n], self._kept[n:])
+            at = self._data - self._kept.data_ptr()
+            data, scales = _mx4_bytes(self.rows, self.cols)
+            self._kept = (self._kept[at:at + data], self._kept[at + data:at + data + scales])
         return self._kept
 
     @property
@@ -148,6 +160,11 @@ class Mx4:
     @property
     def shape(self):
         return self.rows, self.cols
+
+
+def _stream(d):
+    """Handle of the device's current stream, without a stream object around it where torch has that."""
+    return _raw_stream(d.index) if _raw_stream is not None else torch.cuda.current_stream(d).cuda_stream
 
 
 def _mx4(q, what):
@@ -175,18 +192,21 @@ def mx4_quantize(x: torch.Tensor, both: bool = False):
     x = _matrix(x, "mx4_quantize")
     d = _one_device("mx4_quantize", x)
     rows, cols = x.shape
+    if both:
+        q, t = Mx4._new(rows, cols, d, True)
+        _check(lib().gecc_mx4_quantize(x.data_ptr(), _DTYPES[x.dtype], rows, cols, _ld(x), q._data, q._scales, t._data, t._scales, _stream(d)))
+        return q, t
     q = Mx4._new(rows, cols, d)
-    t = Mx4._new(cols, rows, d) if both else None
-    _check(lib().gecc_mx4_quantize(x.data_ptr(), _DTYPES[x.dtype], rows, cols, _ld(x), q._data, q._scales, t._data if both else 0,
-                                   t._scales if both else 0, _stream()))
-    return (q, t) if both else q
+    _check(lib().gecc_mx4_quantize(x.data_ptr(), _DTYPES[x.dtype], rows, cols, _ld(x), q._data, q._scales, 0, 0, _stream(d)))
+    return q
 
 
 def mx4_dequantize(q: Mx4, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values of an Mx4 matrix (exact in both types)."""
     _mx4(q, "mx4_dequantize")
-    out = _output(out, q.shape, dtype, _one_device("mx4_dequantize", q), "mx4_dequantize")
-    _check(lib().gecc_mx4_dequantize(q._data, q._scales, q.rows, q.cols, out.data_ptr(), _DTYPES[out.dtype], _ld(out), _stream()))
+    d = _one_device("mx4_dequantize", q)
+    out = _output(out, (q.rows, q.cols), dtype, d, "mx4_dequantize")
+    _check(lib().gecc_mx4_dequantize(q._data, q._scales, q.rows, q.cols, out.data_ptr(), _DTYPES[out.dtype], _ld(out), _stream(d)))
     return out
 
 
@@ -199,7 +219,7 @@ def mx4_gemm(a: Mx4, b: Mx4, dtype=torch.float32, out: Optional[torch.Tensor] = 
     n, k, m = a.rows, a.cols, b.rows
     out = _output(out, (n, m), dtype, d, "mx4_gemm")
     ws, at, size = _workspace(_bytes("gecc_mx4_gemm_workspace", n, k, m), d)
-    _check(lib().gecc_mx4_gemm(n, k, m, a._data, a._scales, b._data, b._scales, out.data_ptr(), _DTYPES[out.dtype], _ld(out), at, size, _stream()))
+    _check(lib().gecc_mx4_gemm(n, k, m, a._data, a._scales, b._data, b._scales, out.data_ptr(), _DTYPES[out.dtype], _ld(out), at, size, _stream(d)))
     return out
 
 
@@ -216,7 +236,7 @@ def mx4_linear(x: torch.Tensor, w: Mx4, dtype=None, out: Optional[torch.Tensor] 
         return out
     ws, at, size = _workspace(_bytes("gecc_mx4_linear_workspace", n, k, m), d)
     _check(lib().gecc_mx4_linear(n, k, m, x.data_ptr(), _DTYPES[x.dtype], _ld(x), w._data, w._scales, out.data_ptr(), _DTYPES[out.dtype],
-                                 _ld(out), at, size, _stream()))
+                                 _ld(out), at, size, _stream(d)))
     return out
 
 
@@ -243,7 +263,7 @@ def mx4_linear_backward(dy: torch.Tensor, wt: Optional[Mx4], xt: Optional[Mx4], 
     ws, at, size = _workspace(_bytes("gecc_mx4_linear_backward_workspace", n, k, m), d)
     _check(lib().gecc_mx4_linear_backward(n, k, m, dy.data_ptr(), _DTYPES[dy.dtype], _ld(dy), wt._data if wt else 0, wt._scales if wt else 0,
                                           xt._data if xt else 0, xt._scales if xt else 0, _ptr(dx), _DTYPES[dtype], k, _ptr(dw), k, at, size,
-                                          _stream()))
+                                          _stream(d)))
     return dx, dw
 
 
@@ -273,5 +293,5 @@ def orthogonalize(g: torch.Tensor, momentum: Optional[torch.Tensor] = None, mu: 
                    a=coefficients[0], b=coefficients[1], c=coefficients[2])
     ref = C.byref(p)
     ws, at, size = _workspace(lib().gecc_orthogonalize_workspace(ref), d)
-    _check(lib().gecc_orthogonalize(ref, g.data_ptr(), _ptr(momentum), out.data_ptr(), at, size, _stream()))
+    _check(lib().gecc_orthogonalize(ref, g.data_ptr(), _ptr(momentum), out.data_ptr(), at, size, _stream(d)))
     return out
