@@ -12,7 +12,7 @@ OUT = os.path.join(HERE, "libgecc.so")
 SOURCES = ["scan_kernels.hip", "gemm_kernels.hip", "gemm_f32_kernels.hip", "gemm_bf16_kernels.hip", "decode_kernels.hip",
            "gecc_api.hip", "mx4_kernels.hip",
            "tile_kernels.hip", "tile256_kernels.hip", "orth_kernels.hip",
-           "orth_narrow_kernels.hip", "ops_api.hip"]
+           "orth_narrow_kernels.hip", "orth_band_kernels.hip", "ops_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"),
          "-I" + CSRC, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall",
          "-Wno-unused-function"]

@@ -88,6 +88,8 @@ struct OrthPlan {
   int chunk;                      // batch items that go through all steps together
   TilePlan gram, poly, update;
   size_t q;                       // matrices of up to 64 rows
+  OrthBandPlan band;              // of up to 128
+  size_t band_at;
   size_t parts, x[2], lo[2], gram_at, poly_at, part, total;
   OrthSteps steps;
 };
@@ -155,6 +157,7 @@ bool orth_plan(const gecc_orth_params* p, OrthPlan* o) {
   o->sp = align_up(o->s, 64);
   o->lp = align_up(o->l, 64);
   o->total = 0;
+  o->band.batch = 0;
   if (orth_small_ok(o->s, o->l)) return true;
   if (o->s <= ORTH_NARROW) {
     o->nparts = orth_narrow_parts(o->l, p->batch);
@@ -169,6 +172,16 @@ bool orth_plan(const gecc_orth_params* p, OrthPlan* o) {
   o->nparts = (int)(parts > most ? most : parts);
   // X in its two halves, twice, S and P of the items of a chunk: what the steps read and write stays in the 256 MiB memory-side
   // cache (512 x 512 bf16, 256 items: 3673 us all at once, 2287 in chunks of 64 together with the epilogue by rows)
+  if (orth_band_ok(o->s, o->l, p->steps)) {
+    const OrthBandPlan one = orth_band_plan(o->l, p->batch);
+    const int64_t fit = ORTH_CHUNK_BYTES * p->batch / (int64_t)one.total;
+    o->chunk = fit < 1 ? 1 : fit > p->batch ? p->batch : (int)fit;
+    o->band = orth_band_plan(o->l, o->chunk);
+    o->parts = 0;
+    o->band_at = align_up((size_t)p->batch * o->nparts * sizeof(double), 256);
+    o->total = o->band_at + o->band.total;
+    return true;
+  }
   const int64_t item = 4 * o->sp * o->lp * 2 + 2 * (int64_t)o->s * o->sp * 2;
   const int64_t fit = ORTH_CHUNK_BYTES / item;
   o->chunk = fit < 1 ? 1 : fit > p->batch ? p->batch : (int)fit;
@@ -192,18 +205,28 @@ bool orth_plan(const gecc_orth_params* p, OrthPlan* o) {
   return true;
 }
 
+// the items of a batch from `first` on; returns where their outputs begin
+void* chunk_of(const gecc_orth_params& p, OrthPrepArgs* prep, void* dev_O, int first, int items) {
+  prep->p.batch = items;
+  prep->G = static_cast<const char*>(prep->G) + first * p.stride_g * (int64_t)elem_size(p.dtype);
+  if (prep->M) prep->M += first * p.stride_m;
+  prep->parts += (int64_t)first * prep->nparts;
+  return static_cast<char*>(dev_O) + first * p.stride_o * (int64_t)elem_size(p.out_dtype);
+}
+
+hipError_t band_chunk(const gecc_orth_params& p, const OrthPlan& o, OrthPrepArgs prep, void* dev_O, char* ws, int first, int items, hipStream_t st) {
+  dev_O = chunk_of(p, &prep, dev_O, first, items);
+  return launch_orth_bands(prep, dev_O, o.steps, o.band, ws + o.band_at, st);
+}
+
 // items first .. first + items - 1 through all steps, after the norms of all of them
 hipError_t orth_chunk(const gecc_orth_params& params, const OrthPlan& o, OrthPrepArgs prep, void* dev_O, char* ws, int first, int items, hipStream_t st) {
   const gecc_orth_params* p = &params;
   auto half = [&](size_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
-  prep.p.batch = items;
-  prep.G = static_cast<const char*>(prep.G) + first * p->stride_g * (int64_t)elem_size(p->dtype);
-  if (prep.M) prep.M += first * p->stride_m;
-  prep.parts += (int64_t)first * prep.nparts;
+  dev_O = chunk_of(params, &prep, dev_O, first, items);
   prep.hi = half(o.x[0]);
   prep.lo = half(o.lo[0]);
   hipError_t e = launch_orth_start(prep, st);
-  dev_O = static_cast<char*>(dev_O) + first * p->stride_o * (int64_t)elem_size(p->out_dtype);
 
   const int64_t xs = o.sp * o.lp, qs = (int64_t)o.s * o.sp;     // elements of X, of S and P
   for (int t = 0; t < p->steps && e == hipSuccess; ++t) {
@@ -416,7 +439,7 @@ int gecc_orthogonalize(const gecc_orth_params* p, const void* dev_G, float* dev_
   if (p->steps == 0) return hip_rc(launch_orth_store(prep, dev_O, st));
   for (int first = 0; first < p->batch && e == hipSuccess; first += o.chunk) {
     const int items = p->batch - first < o.chunk ? p->batch - first : o.chunk;
-    e = orth_chunk(*p, o, prep, dev_O, ws, first, items, st);
+    e = o.band.batch ? band_chunk(*p, o, prep, dev_O, ws, first, items, st) : orth_chunk(*p, o, prep, dev_O, ws, first, items, st);
   }
   return hip_rc(e);
 }

@@ -115,6 +115,14 @@ size_t orth_narrow_part_bytes(int s, int nparts, int batch);
 size_t orth_narrow_q_bytes(int s, int batch);
 hipError_t launch_orth_narrow(const OrthPrepArgs& a, void* out, float* q, hipStream_t st);
 // O = scale * X where there are no steps
+// longer matrices with a shorter side of up to 128 (orth_band_kernels.hip)
+struct OrthBandPlan {
+  int bands, groups, batch;      // bands of the long side and workgroups of a matrix, matrices at once
+  size_t ranges[2], sum, total;  // places in the workspace, behind X
+};
+bool orth_band_ok(int s, int l, int steps);
+OrthBandPlan orth_band_plan(int l, int batch);
+hipError_t launch_orth_bands(const OrthPrepArgs& a, void* out, const OrthSteps& steps, const OrthBandPlan& plan, char* ws, hipStream_t st);
 hipError_t launch_orth_store(const OrthPrepArgs& a, void* out, hipStream_t st);
 
 }  // namespace gecc

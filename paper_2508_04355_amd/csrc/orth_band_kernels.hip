@@ -1,0 +1,395 @@
+// The orthogonalised update of long matrices whose shorter side s is more than 64 and at most 128 (formulas: gecc_ops.h).
+//
+// All s x s matrices fit a workgroup, so that one launch is a whole step: a workgroup sums the ranges of S = X X^T that the last
+// launch left, makes P of it (each for itself, 1.2 us), takes its bands of LP elements of the long side through X <- a X + P X
+// and leaves its range of the next S.  X travels in fp32 in the order of the accumulators, one read and one write a step.  Where
+// there are many ranges a launch between two steps adds them up.
+//
+// Bound by latency for one matrix: a step 9 us (its three products in a row 3.6, the rest memory, barriers and the launch), the
+// sums 2 to 4.  Measured (whole call, fp32 with momentum; in brackets the tiles of the larger matrices, four or five launches a
+// step): 128 x 400 65 us (78), 128 x 4096 73 (106), 95 x 2814 85 (107), 128 x 65536 158 (218), 30 of 1000 x 128 120 (122), 256 of
+// 128 x 512 226 (265), 64 of 66 x 4096 368 (519).  Bands of 256 are slower everywhere (128 x 4096 100 us): a step's work in a row is
+// twice as long.
+#include "ops_internal.h"
+#include "ops_device.h"
+#include "lds_limit.h"
+#include "orth_device.h"
+
+namespace gecc {
+namespace {
+
+constexpr int SP = 128, LP = 128, BAND_THREADS = 512, SPITCH = 256;
+// Ranges of S that every workgroup of a step adds up by itself: 64 KiB each (128 x 1000, eight ranges: 78 us, with the launch 68; 100 of
+// 128 x 1024, two: 206, with the launch 224)
+constexpr int BAND_RANGES = 4;
+constexpr int S_VECTORS = SP * SP / 4;             // of S, in f32x4
+constexpr int GI = SP / 32, FJ = SP / 64;          // 16 x 16 blocks of a wavefront of S: GI x FJ
+
+struct OrthBandArgs {
+  OrthPrepArgs prep;
+  OrthSteps steps;
+  void* out;
+  bool vec_out;                  // rows of the output aligned to four elements
+  float* x;                      // [batch][bands][SP * LP], a band in the order of the accumulators
+  const float* ranges;           // [batch][nranges][SP * SP], S of this step
+  float* next;                   // [batch][gridDim.x][SP * SP]
+  int nranges, bands, step;
+};
+
+struct Band {
+  static constexpr int XPITCH = LP * 2, FI = LP / 32, VECTORS = SP * LP / 4, UP = LP + 1;
+  static constexpr int X_BYTES = SP * XPITCH;
+  // S (and P in its place) behind X; U in fp32 in place of both
+  static constexpr int U_BYTES = SP * UP * 4, LDS = X_BYTES + SP * SPITCH, START_LDS = (U_BYTES > LDS ? U_BYTES : LDS) + 64;
+  float x[FI][FJ][4];            // element (short side 16 (FJ wj + j) + l16, long side 16 (FI wi + i) + 4 g + v)
+
+  __device__ __forceinline__ void load(const float* at) {
+    const f32x4_t* p = reinterpret_cast<const f32x4_t*>(at) + (threadIdx.x >> 6) * (FI * FJ * 64) + (threadIdx.x & 63);
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) {
+        const f32x4_t y = p[(i * FJ + j) * 64];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[i][j][v] = y[v];
+      }
+  }
+  __device__ __forceinline__ void store(float* at) const {
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(at) + (threadIdx.x >> 6) * (FI * FJ * 64) + (threadIdx.x & 63);
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) p[(i * FJ + j) * 64] = f32x4_t{x[i][j][0], x[i][j][1], x[i][j][2], x[i][j][3]};
+  }
+  // to LDS in fp16
+  __device__ __forceinline__ void put(char* X) const {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4, wi = wave & 1, wj = wave >> 1;
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) put4<XPITCH>(X, (FJ * wj + j) * 16 + l16, (FI * wi + i) * 16 + 4 * g, x[i][j]);
+  }
+  // S += X X^T of the band in LDS
+  static __device__ __forceinline__ void gram(const char* X, f32x4_t (&s)[GI][FJ]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4, wi = wave & 1, wj = wave >> 1;
+#pragma unroll
+    for (int k = 0; k < LP / 32; ++k) {
+      f16x8_t fa[GI], fb[FJ];
+#pragma unroll
+      for (int i = 0; i < GI; ++i) fa[i] = row_fragment<XPITCH>(X, (GI * wi + i) * 16 + l16, k * 4 + g);
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) fb[j] = row_fragment<XPITCH>(X, (FJ * wj + j) * 16 + l16, k * 4 + g);
+#pragma unroll
+      for (int i = 0; i < GI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) s[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[i], fb[j], s[i][j], 0, 0, 0);
+    }
+  }
+};
+
+__device__ __forceinline__ void clear(f32x4_t (&s)[GI][FJ]) {
+#pragma unroll
+  for (int i = 0; i < GI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) s[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+}
+// a range of S, in the order of the accumulators
+__device__ __forceinline__ void store_range(float* to, const f32x4_t (&s)[GI][FJ]) {
+  f32x4_t* p = reinterpret_cast<f32x4_t*>(to) + (threadIdx.x >> 6) * (GI * FJ * 64) + (threadIdx.x & 63);
+#pragma unroll
+  for (int i = 0; i < GI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) p[(i * FJ + j) * 64] = s[i][j];
+}
+
+// X = x_scale U / (|U| + eps) and the first S
+template <bool BF16G, bool VEC>
+__global__ __launch_bounds__(BAND_THREADS) void orth_band_start_kernel(OrthBandArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const OrthPrepArgs& o = a.prep;
+  const gecc_orth_params& p = o.p;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
+  const int wi = wave & 1, wj = wave >> 1;
+  const int b = blockIdx.y;
+  float* U = reinterpret_cast<float*>(smem);
+  double* red = reinterpret_cast<double*>(smem + Band::START_LDS - 64);
+  double sum = 0.0;
+  for (int q = tid; q < o.nparts; q += BAND_THREADS) sum += o.parts[(int64_t)b * o.nparts + q];
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+  if (lane == 0) red[wave] = sum;
+  __syncthreads();
+  sum = ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
+  const float f = (float)((double)o.x_scale / (sqrt(sum) + (double)p.eps));
+  const float* M = o.M ? o.M + (int64_t)b * p.stride_m : nullptr;
+  f32x4_t s[GI][FJ];
+  clear(s);
+  for (int band = blockIdx.x; band < a.bands; band += gridDim.x) {
+    // pieces of eight columns: SP x LP elements, zeros beyond the matrix
+    const int l0 = band * LP;
+    constexpr int ROUNDS = SP * LP / 8 / BAND_THREADS;
+#pragma unroll 4
+    for (int h = 0; h < ROUNDS; ++h) {
+      const int q = h * BAND_THREADS + tid;
+      const int row = o.tall ? l0 + q / (SP / 8) : q / (LP / 8), c = o.tall ? q % (SP / 8) * 8 : l0 + q % (LP / 8) * 8;
+      const bool ok = row < p.rows && c < p.cols;
+      float y[8], m[8];
+      load_g<BF16G, VEC>(o, b, row, c, ok, y);
+      if (M) {
+        load8<true, VEC>(M, (int64_t)row * p.ld_m + c, c, p.cols, ok, m);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = update_of(o, y[i], m[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float u = ok && c + i < p.cols ? y[i] * f : 0.f;
+        if (o.tall) U[(c + i) * Band::UP + q / (SP / 8)] = u;
+        else U[q / (LP / 8) * Band::UP + q % (LP / 8) * 8 + i] = u;
+      }
+    }
+    __syncthreads();
+    Band x;
+#pragma unroll
+    for (int i = 0; i < Band::FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x.x[i][j][v] = U[((FJ * wj + j) * 16 + l16) * Band::UP + (Band::FI * wi + i) * 16 + 4 * g + v];
+    __syncthreads();
+    x.store(a.x + ((int64_t)b * a.bands + band) * (SP * LP));
+    x.put(smem);
+    __syncthreads();
+    Band::gram(smem, s);
+    __syncthreads();
+  }
+  store_range(a.next + ((int64_t)b * gridDim.x + blockIdx.x) * (SP * SP), s);
+}
+
+// The ranges of S added up in their order, by quarters: 64 vectors a workgroup
+__global__ __launch_bounds__(256) void orth_band_sum_kernel(const float* ranges, float* out, int nranges) {
+  __shared__ f32x4_t part[256];
+  const int tid = threadIdx.x, e = blockIdx.x * 64 + (tid & 63), b = blockIdx.y;
+  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(ranges) + (int64_t)b * nranges * S_VECTORS + e;
+  const int each = (nranges + 3) / 4, first = (tid >> 6) * each, end = first + each < nranges ? first + each : nranges;
+  f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int r = first; r < end; ++r) s += p[(int64_t)r * S_VECTORS];
+  part[tid] = s;
+  __syncthreads();
+  if (tid < 64) reinterpret_cast<f32x4_t*>(out)[(int64_t)b * S_VECTORS + e] = (part[tid] + part[64 + tid]) + (part[128 + tid] + part[192 + tid]);
+}
+
+// One step
+template <bool LAST>
+__global__ __launch_bounds__(BAND_THREADS) void orth_band_step_kernel(OrthBandArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const OrthPrepArgs& o = a.prep;
+  const gecc_orth_params& p = o.p;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
+  const int wi = wave & 1, wj = wave >> 1;
+  const int b = blockIdx.y, t = a.step;
+  const float sx = a.steps.sx[t], ss = a.steps.ss[t], sp = a.steps.sp[t], fold = a.steps.fold[t];
+  char* X = smem;
+  char* S = smem + Band::X_BYTES;
+  float* home = a.x + (int64_t)b * a.bands * (SP * LP);
+  Band x;
+  x.load(home + (int64_t)blockIdx.x * (SP * LP));           // (gridDim.x <= bands)
+  f32x4_t s[GI][FJ], poly[GI][FJ];
+  clear(s);
+  clear(poly);
+  {
+    const f32x4_t* q = reinterpret_cast<const f32x4_t*>(a.ranges) + (int64_t)b * a.nranges * S_VECTORS + wave * (GI * FJ * 64) + lane;
+#pragma unroll 2
+    for (int r = 0; r < a.nranges; ++r)
+#pragma unroll
+      for (int i = 0; i < GI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) s[i][j] += q[(int64_t)r * S_VECTORS + (i * FJ + j) * 64];
+  }
+  const float to_s = ss / (sx * sx);
+#pragma unroll
+  for (int i = 0; i < GI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) {
+      float y[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        y[v] = s[i][j][v] * to_s;
+        s[i][j][v] = (float)(_Float16)y[v];      // the S that both terms of P are made from
+      }
+      put4<SPITCH>(S, (FJ * wj + j) * 16 + l16, (GI * wi + i) * 16 + 4 * g, y);
+    }
+  x.put(X);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < SP / 32; ++k) {
+    f16x8_t fa[GI], fb[FJ];
+#pragma unroll
+    for (int i = 0; i < GI; ++i) fa[i] = row_fragment<SPITCH>(S, (GI * wi + i) * 16 + l16, k * 4 + g);
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) fb[j] = row_fragment<SPITCH>(S, (FJ * wj + j) * 16 + l16, k * 4 + g);
+#pragma unroll
+    for (int i = 0; i < GI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) poly[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[i], fb[j], poly[i][j], 0, 0, 0);
+  }
+  __syncthreads();
+  const float of_s = p.b * (sp / ss), of_ss = p.c * (sp / (ss * ss)), eye = fold * p.a * sp;
+#pragma unroll
+  for (int i = 0; i < GI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) {
+      float y[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        y[v] = fmaf(of_s, s[i][j][v], of_ss * poly[i][j][v]);
+        if ((GI * wi + i) * 16 + 4 * g + v == (FJ * wj + j) * 16 + l16) y[v] += eye;
+      }
+      put4<SPITCH>(S, (FJ * wj + j) * 16 + l16, (GI * wi + i) * 16 + 4 * g, y);
+    }
+  __syncthreads();
+  const float to = LAST ? p.scale : a.steps.sx[t + 1], of_x = (1.f - fold) * p.a * (to / sx), of_px = to / (sp * sx);
+  clear(s);
+  for (int band = blockIdx.x; band < a.bands; band += gridDim.x) {
+    if (band != (int)blockIdx.x) {
+      x.load(home + (int64_t)band * (SP * LP));
+      x.put(X);
+      __syncthreads();
+    }
+    f32x4_t acc[Band::FI][FJ];
+#pragma unroll
+    for (int i = 0; i < Band::FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < SP / 32; ++k) {
+      f16x8_t fb[FJ];
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) fb[j] = row_fragment<SPITCH>(S, (FJ * wj + j) * 16 + l16, k * 4 + g);
+#pragma unroll
+      for (int i = 0; i < Band::FI; ++i) {
+        const f16x8_t fa = column_fragment<Band::XPITCH>(X, k * 32, (Band::FI * wi + i) * 16);
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa, fb[j], acc[i][j], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < Band::FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x.x[i][j][v] = fmaf(of_x, x.x[i][j][v], of_px * acc[i][j][v]);
+    __syncthreads();                              // X is free again
+    if (!LAST) {
+      x.store(home + (int64_t)band * (SP * LP));
+      x.put(X);
+      __syncthreads();
+      Band::gram(X, s);
+      __syncthreads();
+      continue;
+    }
+#pragma unroll
+    for (int i = 0; i < Band::FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) {
+        const int is = (FJ * wj + j) * 16 + l16;
+        const int64_t il = (int64_t)band * LP + (Band::FI * wi + i) * 16 + 4 * g;
+        if (is >= o.s) continue;
+        const int64_t at = (int64_t)b * p.stride_o + (o.tall ? il * p.ld_o + is : is * p.ld_o + il);
+        const float (&y)[4] = x.x[i][j];
+        if (a.vec_out && !o.tall && il + 4 <= o.l) {
+          if (p.out_dtype == GECC_F32) *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + at) = f32x4_t{y[0], y[1], y[2], y[3]};
+          else *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(a.out) + at) =
+                   u32x2_t{(unsigned)to_bf16(y[0]) | ((unsigned)to_bf16(y[1]) << 16), (unsigned)to_bf16(y[2]) | ((unsigned)to_bf16(y[3]) << 16)};
+          continue;
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          if (il + v >= o.l) continue;
+          const int64_t place = at + v * (o.tall ? p.ld_o : 1);
+          if (p.out_dtype == GECC_F32) static_cast<float*>(a.out)[place] = y[v];
+          else static_cast<uint16_t*>(a.out)[place] = to_bf16(y[v]);
+        }
+      }
+  }
+  if (!LAST) store_range(a.next + ((int64_t)b * gridDim.x + blockIdx.x) * (SP * SP), s);
+}
+
+template <typename K>
+hipError_t raised(K kern, LdsLimit& limit, int lds) {
+  return lds > 65536 ? limit.raise(reinterpret_cast<const void*>(kern), lds) : hipSuccess;
+}
+template <bool BF16G, bool VEC>
+hipError_t start(const OrthBandArgs& a, const dim3& grid, hipStream_t st) {
+  static LdsLimit limit;
+  const hipError_t e = raised(orth_band_start_kernel<BF16G, VEC>, limit, Band::START_LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((orth_band_start_kernel<BF16G, VEC>), grid, dim3(BAND_THREADS), Band::START_LDS, st, a);
+  return hipGetLastError();
+}
+template <bool LAST>
+hipError_t step(const OrthBandArgs& a, const dim3& grid, hipStream_t st) {
+  static LdsLimit limit;
+  const hipError_t e = raised(orth_band_step_kernel<LAST>, limit, Band::LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((orth_band_step_kernel<LAST>), grid, dim3(BAND_THREADS), Band::LDS, st, a);
+  return hipGetLastError();
+}
+
+hipError_t bands(const OrthPrepArgs& prep, void* out, const OrthSteps& steps, const OrthBandPlan& plan, char* ws, hipStream_t st) {
+  OrthBandArgs a{};
+  a.prep = prep;
+  a.steps = steps;
+  a.out = out;
+  a.vec_out = orth_vec_out(prep, out);
+  a.x = reinterpret_cast<float*>(ws);
+  a.bands = plan.bands;
+  float* ranges[2] = {reinterpret_cast<float*>(ws + plan.ranges[0]), reinterpret_cast<float*>(ws + plan.ranges[1])};
+  float* sum = reinterpret_cast<float*>(ws + plan.sum);
+  const dim3 grid(plan.groups, prep.p.batch);
+  const bool vec = vectors_ok(prep), bf16 = prep.p.dtype == GECC_BF16;
+  a.next = ranges[0];
+  hipError_t e = bf16 ? (vec ? start<true, true>(a, grid, st) : start<true, false>(a, grid, st))
+                      : (vec ? start<false, true>(a, grid, st) : start<false, false>(a, grid, st));
+  for (int t = 0; t < prep.p.steps && e == hipSuccess; ++t) {
+    a.step = t;
+    a.ranges = ranges[t & 1];
+    a.nranges = plan.groups;
+    a.next = ranges[(t + 1) & 1];
+    if (plan.groups > BAND_RANGES) {
+      hipLaunchKernelGGL(orth_band_sum_kernel, dim3(S_VECTORS / 64, prep.p.batch), dim3(256), 0, st, a.ranges, sum, plan.groups);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      a.ranges = sum;
+      a.nranges = 1;
+    }
+    e = t + 1 == prep.p.steps ? step<true>(a, grid, st) : step<false>(a, grid, st);
+  }
+  return e;
+}
+
+}  // namespace
+
+bool orth_band_ok(int s, int l, int steps) { return s > ORTH_NARROW && s <= SP && !orth_small_ok(s, l) && steps > 0; }
+
+OrthBandPlan orth_band_plan(int l, int batch) {
+  OrthBandPlan plan{};
+  plan.batch = batch;
+  plan.bands = (l + LP - 1) / LP;
+  // one workgroup a compute unit in all (up to twice as many: 128 x 65536 197 us instead of 158)
+  const int most = batch >= 256 ? 1 : 256 / batch;
+  plan.groups = plan.bands < most ? plan.bands : most;
+  const size_t x = (size_t)batch * plan.bands * SP * LP * 4, s = (size_t)batch * SP * SP * 4;
+  plan.ranges[0] = x;
+  plan.ranges[1] = plan.ranges[0] + s * plan.groups;
+  plan.sum = plan.ranges[1] + s * plan.groups;
+  plan.total = plan.sum + (plan.groups > BAND_RANGES ? s : 0);
+  return plan;
+}
+
+hipError_t launch_orth_bands(const OrthPrepArgs& prep, void* out, const OrthSteps& steps, const OrthBandPlan& plan, char* ws, hipStream_t st) {
+  if (!orth_band_ok(prep.s, prep.l, prep.p.steps) || prep.p.batch > plan.batch) return hipErrorInvalidValue;
+  return bands(prep, out, steps, plan, ws, st);
+}
+
+}  // namespace gecc

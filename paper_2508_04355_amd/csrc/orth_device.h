@@ -1,4 +1,5 @@
-// What the kernels of the orthogonalised update share: U from the gradient and the momentum, alignment rules.
+// What the kernels of the orthogonalised update share: U from the gradient and the momentum, alignment rules, matrices of fp16
+// in LDS.
 #pragma once
 #include "ops_internal.h"
 #include "ops_device.h"
@@ -26,6 +27,38 @@ bool vectors_ok(const OrthPrepArgs& a) {
 inline bool orth_vec_out(const OrthPrepArgs& a, const void* out) {
   const int es = a.p.out_dtype == GECC_F32 ? 4 : 2;
   return reinterpret_cast<uintptr_t>(out) % (4 * es) == 0 && a.p.ld_o % 4 == 0 && (a.p.batch == 1 || a.p.stride_o % 4 == 0);
+}
+
+// fp16 matrices in LDS: the sixteen 16-byte chunks of 256 bytes of a row are XOR-swizzled by the row
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(8))) short s16x8_t;
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+__device__ __forceinline__ int swizzle(int row, int chunk) {
+  return chunk ^ (((row & 3) << 1) | (row & 8) | ((row >> 2) & 1));
+}
+template <int PITCH>
+__device__ __forceinline__ f16x8_t row_fragment(const char* m, int row, int chunk) {
+  return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const s16x8_t*>(m + row * PITCH + (swizzle(row, chunk) << 4)));
+}
+// 16 columns from `col` on, rows `row` .. `row` + 31
+template <int PITCH>
+__device__ __forceinline__ f16x8_t column_fragment(const char* m, int row, int col) {
+  const int lane = threadIdx.x & 63;
+  const int r = row + 8 * (lane >> 4) + ((lane >> 2) & 3), c = col + (lane & 3) * 4;
+  const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(m + r * PITCH + (swizzle(r, c >> 3) << 4) + (c & 7) * 2));
+  const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(m + (r + 4) * PITCH + (swizzle(r + 4, c >> 3) << 4) + (c & 7) * 2));
+  return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// four fp16 values of row `row` from column `col` (a multiple of 4) on
+template <int PITCH>
+__device__ __forceinline__ void put4(char* m, int row, int col, const float (&x)[4]) {
+  f16x4_t h;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) h[v] = (_Float16)x[v];
+  *reinterpret_cast<f16x4_t*>(m + row * PITCH + (swizzle(row, col >> 3) << 4) + (col & 7) * 2) = h;
 }
 
 }  // namespace

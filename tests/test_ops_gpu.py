@@ -360,6 +360,79 @@ def test_strided_gradients_momenta_and_outputs():
         assert bool((big_m == 5.0).all()) and bool((big_o == 5.0).all())
 
 
+# ---- ... of long matrices with a shorter side of 65 to 128: bands of 128 of the long side, a launch a step ----------------------
+@pytest.mark.parametrize("kind", ["noise", "spiked", "rank"])
+@pytest.mark.parametrize("rows,cols", [(65, 257), (128, 512), (100, 513), (96, 1000), (1001, 127), (700, 66), (128, 4096), (3000, 77)])
+def test_bands(rows, cols, kind):
+    rng = _rng(rows, cols, 14)
+    g, t = _store(1e-3 * _gradient(rng, rows, cols, kind), "bf16")
+    want, _ = R.orthogonalise(g, None, 0.0, True, 5, COEF, 1e-7, 0.7)
+    _orth_check(ops.orthogonalize(t, scale=0.7), want, "bf16")
+    _orth_check(ops.orthogonalize(t, scale=0.7, dtype=torch.float32), want, "f32")
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 8])
+@pytest.mark.parametrize("rows,cols", [(90, 300), (2000, 128)])
+def test_bands_steps(rows, cols, steps):
+    rng = _rng(rows, cols, steps, 15)
+    g, t = _store(_gradient(rng, rows, cols, "spiked"), "f32")
+    want, _ = R.orthogonalise(g, None, 0, True, steps, COEF, 1e-7, 2.0)
+    _orth_check(ops.orthogonalize(t, steps=steps, scale=2.0, dtype=torch.float32), want, "f32")
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(70, 1025), (600, 128)])
+def test_bands_momentum(rows, cols, dtype, nesterov):
+    rng = _rng(rows, cols, 16)
+    m = torch.zeros(rows, cols, device=DEV)
+    ref = np.zeros((rows, cols))
+    for _ in range(3):
+        g, t = _store(_gradient(rng, rows, cols, "spiked"), dtype)
+        o = ops.orthogonalize(t, momentum=m, mu=0.9, nesterov=nesterov)
+        want, ref = R.orthogonalise(g, ref, float(np.float32(0.9)), nesterov, 5, COEF, 1e-7, 1.0)
+        _orth_check(o, want, "bf16")
+        assert np.abs(m.double().cpu().numpy() - ref).max() <= 3 * 2.0 ** -24 * np.abs(ref).max()     # a rounding a step
+
+
+# several bands a workgroup (more than 256 of them), and more items than go through the steps together (about 192 MiB of them)
+@pytest.mark.parametrize("batch,rows,cols", [(3, 70, 600), (40, 128, 1500), (300, 66, 400), (1000, 65, 257)])
+def test_bands_batches(batch, rows, cols):
+    rng = _rng(batch, rows, cols, 17)
+    g = torch.from_numpy(rng.standard_normal((batch, rows, cols)).astype(np.float32)).to(DEV)
+    kept = g.clone()
+    o = ops.orthogonalize(g, dtype=torch.float32)
+    assert torch.equal(g, kept)
+    for i in sorted({0, 1, batch // 2, batch // 2 + 1, batch - 2, batch - 1}):
+        want, _ = R.orthogonalise(g[i].double().cpu().numpy(), None, 0.0, True, 5, COEF, 1e-7, 1.0)
+        _orth_check(o[i], want, "f32")
+    # S = X X^T after the steps has a trace of about the rank: none of the items between was left out
+    trace = o.square().sum((1, 2))
+    assert bool((trace > 0.4 * min(rows, cols)).all()) and bool((trace < 1.6 * min(rows, cols)).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(80, 290), (290, 80)])
+def test_bands_strides_zeros_and_no_number(rows, cols):
+    big = torch.randn(2, rows + 3, cols + 5, device=DEV)
+    m0 = torch.randn(2, rows + 1, cols + 2, device=DEV)
+    g, m = big[:, 1:rows + 1, 3:cols + 3], m0[:, :rows, 1:cols + 1]
+    out = torch.full((2, rows + 2, cols + 7), 7.0, device=DEV)
+    dense_m = m.contiguous()
+    want = ops.orthogonalize(g.contiguous(), momentum=dense_m, dtype=torch.float32)
+    before = m0.clone()
+    ops.orthogonalize(g, momentum=m, out=out[:, 2:, 1:cols + 1])
+    torch.testing.assert_close(out[:, 2:, 1:cols + 1], want, rtol=0, atol=1e-5)      # (another order of the norm's sum)
+    assert torch.equal(m, dense_m)
+    out[:, 2:, 1:cols + 1] = 7.0
+    assert bool((out == 7.0).all())
+    m0[:, :rows, 1:cols + 1] = before[:, :rows, 1:cols + 1]
+    assert torch.equal(m0, before)
+    z = torch.zeros(2, rows, cols, device=DEV)
+    z[1, 3, 4] = float("nan")
+    o = ops.orthogonalize(z, dtype=torch.float32)
+    assert bool((o[0] == 0).all()) and bool(o[1].isnan().all())
+
+
 def test_orthogonalize_refuses():
     g = torch.zeros(4, 6, device=DEV)
     for f in (lambda: ops.orthogonalize(g.double()), lambda: ops.orthogonalize(g[0]), lambda: ops.orthogonalize(g, momentum=g.bfloat16()),
