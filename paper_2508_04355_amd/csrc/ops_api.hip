@@ -33,15 +33,8 @@ TilePlan product_plan(int32_t n, int32_t k, int32_t m) {
 size_t product_workspace(int32_t n, int32_t k, int32_t m) {
   return n <= MX_FEW_ROWS ? 0 : align_up(product_plan(n, k, m).part_bytes, 256);
 }
-hipError_t product(int32_t n, int32_t k, int32_t m, const uint8_t* a_data, const uint8_t* a_scales, const uint8_t* b_data,
-                   const uint8_t* b_scales, void* C, int32_t c_dtype, int64_t ldc, void* ws, hipStream_t st) {
-  if (n <= MX_FEW_ROWS) {
-    MxFewArgs f{};
-    f.n = n; f.k = k; f.m = m;
-    f.x_data = a_data; f.x_scales = a_scales; f.w_data = b_data; f.w_scales = b_scales;
-    f.y = C; f.y_dtype = c_dtype; f.ldy = ldc;
-    return launch_mx4_few(f, st);
-  }
+TileArgs product_args(int32_t n, int32_t k, int32_t m, const uint8_t* a_data, const uint8_t* a_scales, const uint8_t* b_data,
+                      const uint8_t* b_scales, void* C, int32_t c_dtype, int64_t ldc, void* ws) {
   TileArgs t{};
   // (the stored side of a lane's four values is the tile's first operand: the columns of C)
   t.A = b_data; t.B = a_data;
@@ -52,7 +45,18 @@ hipError_t product(int32_t n, int32_t k, int32_t m, const uint8_t* a_data, const
   t.batch = 1;
   t.part = static_cast<float*>(ws);
   t.out = C; t.ldo = ldc; t.out_dtype = c_dtype;
-  return launch_tiles(KIND_MX4, EPI_OUT, t, product_plan(n, k, m), st);
+  return t;
+}
+hipError_t product(int32_t n, int32_t k, int32_t m, const uint8_t* a_data, const uint8_t* a_scales, const uint8_t* b_data,
+                   const uint8_t* b_scales, void* C, int32_t c_dtype, int64_t ldc, void* ws, hipStream_t st) {
+  if (n <= MX_FEW_ROWS) {
+    MxFewArgs f{};
+    f.n = n; f.k = k; f.m = m;
+    f.x_data = a_data; f.x_scales = a_scales; f.w_data = b_data; f.w_scales = b_scales;
+    f.y = C; f.y_dtype = c_dtype; f.ldy = ldc;
+    return launch_mx4_few(f, st);
+  }
+  return launch_tiles(KIND_MX4, EPI_OUT, product_args(n, k, m, a_data, a_scales, b_data, b_scales, C, c_dtype, ldc, ws), product_plan(n, k, m), st);
 }
 
 struct LinearLayout { size_t x_data, x_scales, part, total; bool raw; };
@@ -397,6 +401,13 @@ int gecc_mx4_linear_backward(int32_t n, int32_t k, int32_t m, const void* dev_dY
   if (dev_dX) { q.data = ws; q.scales = ws + l.q_scales; }
   if (dev_dW) { q.t_data = ws + l.t_data; q.t_scales = ws + l.t_scales; }
   hipError_t e = launch_mx4_quantize(q, st);
+  if (e == hipSuccess && dev_dX && dev_dW && n > MX_FEW_ROWS && m > MX_FEW_ROWS) {
+    e = launch_tiles_pair(product_args(n, m, k, ws, ws + l.q_scales, static_cast<const uint8_t*>(dev_Wt_data), static_cast<const uint8_t*>(dev_Wt_scales),
+                                       dev_dX, dx_dtype, lddx, ws + l.part), product_plan(n, m, k),
+                          product_args(m, n, k, ws + l.t_data, ws + l.t_scales, static_cast<const uint8_t*>(dev_Xt_data),
+                                       static_cast<const uint8_t*>(dev_Xt_scales), dev_dW, GECC_F32, lddw, ws + l.part), product_plan(m, n, k), st);
+    return hip_rc(e);
+  }
   if (e == hipSuccess && dev_dX)
     e = product(n, m, k, ws, ws + l.q_scales, static_cast<const uint8_t*>(dev_Wt_data), static_cast<const uint8_t*>(dev_Wt_scales), dev_dX,
                 dx_dtype, lddx, ws + l.part, st);

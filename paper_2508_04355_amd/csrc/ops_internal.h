@@ -83,6 +83,7 @@ TilePlan plan_tiles(TileKind kind, TileEpi epi, int64_t m_rows, int64_t n_rows, 
 // 32-bit offsets inside an operand: 256 rows of `row_bytes`; k_rows of them where its rows are contiguous
 inline bool tile256_ok(int64_t row_bytes, int64_t k_rows) { return 256 * row_bytes < 0x7fffffff && k_rows * row_bytes < 0x7fffffff; }
 hipError_t launch_tiles_256(TileKind kind, TileEpi epi, const TileArgs& a, hipStream_t st);     // tile256_kernels.hip
+hipError_t launch_tiles_pair(TileArgs x, const TilePlan& px, TileArgs y, const TilePlan& py, hipStream_t st);   // of 4-bit operands, independent
 hipError_t launch_tiles(TileKind kind, TileEpi epi, const TileArgs& a, const TilePlan& plan, hipStream_t st);
 
 // ---- the orthogonalised update -------------------------------------------------------------------------

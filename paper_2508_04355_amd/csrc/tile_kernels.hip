@@ -120,8 +120,9 @@ __device__ __forceinline__ void tile_at(const TileArgs& a, int t, int& tm, int& 
 
 // RING: stages of LDS.  Bound by latency where there are few tiles: 3001 x 801 X X^T 12.7 us (91 tiles, 47 stages each), its
 // polynomial 6.8, P X 11.8 to 13; 4-bit 2048 x 4096 x 4096 in tiles of 128 19.9 us, 3.5 PFLOP/s.  Others: plan_tiles below.
+// One range of one of the `tiles` tiles of a batch item.
 template <int KIND, bool KCA, int T, int RING, int EPI>
-__global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_out) {
+__device__ __forceinline__ void tile_product(const TileArgs& a, bool vec_out, int b, int tile, int tiles, int range) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int F = T / 32;                       // 16-row fragments of a wavefront, an operand
   constexpr int STAGE = T * 128;                  // bytes of a stage, an operand
@@ -130,9 +131,6 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int wr = wave >> 1, wc = wave & 1, l16 = lane & 15, g = lane >> 4;
-  unsigned group = blockIdx.x + gridDim.x * blockIdx.y, item = 0;
-  if (gridDim.z > 1) batch_place(gridDim.x * gridDim.y, gridDim.z, group + gridDim.x * gridDim.y * blockIdx.z, group, item);
-  const int b = item, tile = group % gridDim.x, range = group / gridDim.x;
   int tm, tn;
   tile_at<T>(a, tile, tm, tn);
   const int r0 = tm * T, c0 = tn * T;
@@ -272,7 +270,7 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
 
   if (a.split > 1) {
     // [batch][tile][range][fragment pair][lane] in the order of the registers; tile_finish_kernel adds the ranges up
-    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + (((int64_t)b * gridDim.x + tile) * a.split + range) * (T * T / 4) + wave * (F * F * 64) + lane;
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + (((int64_t)b * tiles + tile) * a.split + range) * (T * T / 4) + wave * (F * F * 64) + lane;
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
@@ -282,6 +280,21 @@ __global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_o
   __syncthreads();               // the stages are done with: their LDS holds rows of the result now
   store_tile<EPI, F, F>(a, b, acc, reinterpret_cast<float*>(smem) + wave * store_floats<F>(), r0 + wr * (T / 2), c0 + wc * (T / 2), r0 + T, c0 + T,
                          a.symmetric && tm != tn, vec_out);
+}
+
+template <int KIND, bool KCA, int T, int RING, int EPI>
+__global__ __launch_bounds__(THREADS, 2) void tile_kernel(TileArgs a, bool vec_out) {
+  unsigned group = blockIdx.x + gridDim.x * blockIdx.y, item = 0;
+  if (gridDim.z > 1) batch_place(gridDim.x * gridDim.y, gridDim.z, group + gridDim.x * gridDim.y * blockIdx.z, group, item);
+  tile_product<KIND, KCA, T, RING, EPI>(a, vec_out, item, group % gridDim.x, gridDim.x, group / gridDim.x);
+}
+
+// Two products that need not wait for each other, `first` tiles of the one and then the other's: small ones run side by side
+struct TileArgs2 { TileArgs of[2]; bool vec_out[2]; };
+template <int KIND, int T, int RING>
+__global__ __launch_bounds__(THREADS, 2) void tile_pair_kernel(TileArgs2 a, int first) {
+  const int which = (int)blockIdx.x >= first;
+  tile_product<KIND, true, T, RING, EPI_OUT>(a.of[which], a.vec_out[which], 0, (int)blockIdx.x - (which ? first : 0), 0, 0);
 }
 
 // Adds the ranges of a split product up, in their order, and stores the result: a wavefront per fragment pair.
@@ -321,13 +334,18 @@ hipError_t launch_finish(const TileArgs& a, int64_t tiles, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <int KIND, int T, int RING>
+constexpr int lds_bytes() {
+  constexpr int stages = RING * 2 * T * 128 + (KIND == KIND_MX4 ? RING / 2 * 2 * T * 16 : 0), rows = 4 * store_floats<T / 32>() * 4;
+  return stages > rows ? stages : rows;                         // (the epilogue has it afterwards)
+}
+
 template <int KIND, bool KCA, int T, int RING, int EPI>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
   static_assert(RING % 2 == 0 && (RING & (RING - 1)) == 0, "slots of stages, and of their scales, by number");
   const int64_t tiles = tiles_of(a.m_rows, a.n_rows, T, a.symmetric);
   if (tiles > 0x7fffffff || a.batch > 65535) return hipErrorInvalidValue;
-  constexpr int stages = RING * 2 * T * 128 + (KIND == KIND_MX4 ? RING / 2 * 2 * T * 16 : 0), rows = 4 * store_floats<T / 32>() * 4;
-  constexpr int lds = stages > rows ? stages : rows;            // (the epilogue has it afterwards)
+  constexpr int lds = lds_bytes<KIND, T, RING>();
   auto kern = tile_kernel<KIND, KCA, T, RING, EPI>;
   if (lds > 65536) {
     static LdsLimit limit;
@@ -418,6 +436,38 @@ hipError_t launch_any(const TileArgs& a, const TilePlan& plan, hipStream_t st) {
   return groups <= 512 ? launch<KIND, KCA, 64, 4, EPI>(a, st) : launch<KIND, KCA, 64, 2, EPI>(a, st);
 }
 }  // namespace
+
+namespace {
+template <int T, int RING>
+hipError_t launch_pair(const TileArgs& x, const TileArgs& y, int64_t first, int64_t second, hipStream_t st) {
+  constexpr int lds = lds_bytes<KIND_MX4, T, RING>();
+  auto kern = tile_pair_kernel<KIND_MX4, T, RING>;
+  if (lds > 65536) {
+    static LdsLimit limit;
+    const hipError_t e = limit.raise(reinterpret_cast<const void*>(kern), lds);
+    if (e != hipSuccess) return e;
+  }
+  const TileArgs2 a = {{x, y}, {vectors_out(x, 8), vectors_out(y, 8)}};
+  hipLaunchKernelGGL(kern, dim3((unsigned)(first + second)), dim3(THREADS), lds, st, a, (int)first);
+  return hipGetLastError();
+}
+}  // namespace
+
+// Both in one launch where together they are no more workgroups than run at once (the gradients of 1000 x 777 -> 1100, 208 and 234
+// tiles of 64: forward and backward 39.4 -> 35.9 us; tiles of 128 are chosen where there are more than 512 of 64, so that a pair of
+// them is more than 256)
+hipError_t launch_tiles_pair(TileArgs x, const TilePlan& px, TileArgs y, const TilePlan& py, hipStream_t st) {
+  const int64_t first = tiles_of(x.m_rows, x.n_rows, px.tile, false), second = tiles_of(y.m_rows, y.n_rows, py.tile, false);
+  if (px.tile != py.tile || px.tile == 256 || px.split > 1 || py.split > 1 || first + second > 512) {
+    const hipError_t e = launch_tiles(KIND_MX4, EPI_OUT, x, px, st);
+    return e != hipSuccess ? e : launch_tiles(KIND_MX4, EPI_OUT, y, py, st);
+  }
+  x.split = y.split = 1;
+  x.whole = (int)first; y.whole = (int)second;
+  x.symmetric = y.symmetric = false;
+  if (px.tile == 64) return launch_pair<64, 4>(x, y, first, second, st);
+  return launch_pair<128, 2>(x, y, first, second, st);
+}
 
 hipError_t launch_tiles(TileKind kind, TileEpi epi, const TileArgs& a0, const TilePlan& plan, hipStream_t st) {
   TileArgs a = a0;

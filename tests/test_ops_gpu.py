@@ -209,6 +209,18 @@ def test_gradients(n, k, m, dtype):
     assert none is None and torch.equal(one, dw)
 
 
+# tiles of 64 and of 128 in one launch for both gradients, and pairs that do not go together (other tiles, shared ranges, too many)
+@pytest.mark.parametrize("n,k,m", [(65, 1, 65), (130, 70, 1000), (2100, 1400, 2100), (2048, 4096, 80), (4096, 100, 4096)])
+def test_gradients_side_by_side(n, k, m):
+    x, w, dy = (torch.randn(*s, device=DEV, dtype=torch.bfloat16) for s in ((n, k), (m, k), (n, m)))
+    _, qwt = ops.mx4_quantize(w, both=True)
+    _, qxt = ops.mx4_quantize(x, both=True)
+    dx, dw = ops.mx4_linear_backward(dy, qwt, qxt)
+    q, qt = ops.mx4_quantize(dy, both=True)
+    assert torch.equal(dx, ops.mx4_gemm(q, qwt, dtype=torch.bfloat16)) and torch.equal(dw, ops.mx4_gemm(qt, qxt, dtype=torch.float32))
+    assert bool(dx.isfinite().all()) and float(dx.float().norm()) > 0 and float(dw.norm()) > 0
+
+
 def test_gradients_by_differences():
     """Operands that the format holds exactly in both directions (magnitudes 1 to 6 of one scale): the loss
     <dy, x w^T> is then linear, and its differences along a direction that stays on the grid are the gradients'."""
