@@ -119,9 +119,14 @@ struct StepMatrices {
     block_at(q, bi, bj);
     const double* px = x + (16 * bi + l16) * P + lg;
     const double* py = y + (16 * bj + l16) * P + lg;
+    // all reads on their way before the first instruction (in turn with them the steps of 64 x 400 took 60 us instead of 57)
+    double vx[SP / 4], vy[SP / 4];
+#pragma unroll
+    for (int k = 0; k < SP / 4; ++k) { vx[k] = px[4 * k]; vy[k] = py[4 * k]; }
+    __builtin_amdgcn_sched_barrier(0);
     f64x4_t d = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-    for (int k = 0; k < SP; k += 4) d = __builtin_amdgcn_mfma_f64_16x16x4f64(px[k], py[k], d, 0, 0, 0);
+    for (int k = 0; k < SP / 4; ++k) d = __builtin_amdgcn_mfma_f64_16x16x4f64(vx[k], vy[k], d, 0, 0, 0);
     return d;
   }
   // both triangles
@@ -147,15 +152,23 @@ __global__ __launch_bounds__(STEP_THREADS) void narrow_steps_kernel(OrthPrepArgs
   double *S = mem, *T = mem + SP * P, *Q = mem + 2 * SP * P;
   const int b = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
   const double* parts = a.parts + (int64_t)b * nparts * (NB * 256);
-  for (int e = tid; e < NB * 256; e += STEP_THREADS) {
-    double s = 0.0;
-#pragma unroll 8
-    for (int p = 0; p < nparts; ++p) s += parts[(int64_t)p * (NB * 256) + e];
+  constexpr int EACH = (NB * 256 + STEP_THREADS - 1) / STEP_THREADS;
+  double sums[EACH];
+#pragma unroll
+  for (int n = 0; n < EACH; ++n) sums[n] = 0.0;
+#pragma unroll 4
+  for (int p = 0; p < nparts; ++p)
+#pragma unroll
+    for (int n = 0; n < EACH; ++n) sums[n] += parts[(int64_t)p * (NB * 256) + min(tid + n * STEP_THREADS, NB * 256 - 1)];
+#pragma unroll
+  for (int n = 0; n < EACH; ++n) {
+    const int e = tid + n * STEP_THREADS;
+    if (e >= NB * 256) break;
     int bi, bj;
     block_at(e >> 8, bi, bj);
     const int r = 16 * bi + ((e >> 4) & 15), c = 16 * bj + (e & 15);
-    S[r * P + c] = s;
-    if (bi != bj) S[c * P + r] = s;
+    S[r * P + c] = sums[n];
+    if (bi != bj) S[c * P + r] = sums[n];
   }
   for (int e = tid; e < SP * SP; e += STEP_THREADS) Q[e / SP * P + e % SP] = e / SP == e % SP ? 1.0 : 0.0;
   __syncthreads();
@@ -182,21 +195,22 @@ __global__ __launch_bounds__(STEP_THREADS) void narrow_steps_kernel(OrthPrepArgs
         d[n][v] = fma(cc, d[n][v], cb * S[r * P + c]) + (r == c ? ca : 0.0);
       }
       M::put(T, q, d[n]);
+      if (t == 0) M::put(Q, q, d[n]);                // (T I)
     }
     __syncthreads();
     const bool last = t + 1 == a.p.steps;
     // T Q, and S T into the place of S
-    const int blocks = last ? NB : 2 * NB;
+    const int none = t == 0 ? NB : 0, blocks = last ? NB : 2 * NB;
 #pragma unroll
     for (int n = 0; n < MINE2; ++n) {
-      const int q = wave + n * WAVES;
+      const int q = none + wave + n * WAVES;
       if (q >= blocks) break;
       d[n] = q < NB ? M::block(T, Q, q) : M::block(S, T, q - NB);
     }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < MINE2; ++n) {
-      const int q = wave + n * WAVES;
+      const int q = none + wave + n * WAVES;
       if (q >= blocks) break;
       M::put(q < NB ? Q : S, q < NB ? q : q - NB, d[n]);
     }
@@ -228,7 +242,8 @@ __global__ __launch_bounds__(256) void narrow_apply_kernel(OrthPrepArgs a, int t
   __shared__ float Q[SP * QP];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lg = lane >> 4;
   const float* q = q_in + (int64_t)b * (SP * SP + 4);
-  for (int e = tid; e < SP * SP; e += 256) Q[e / SP * QP + e % SP] = q[e];
+#pragma unroll
+  for (int h = 0; h < SP * SP / 256; ++h) Q[(h * 256 + tid) / SP * QP + tid % SP] = q[h * 256 + tid];
   const float f = q[SP * SP];
   for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
     __syncthreads();
