@@ -372,6 +372,17 @@ def test_strided_gradients_momenta_and_outputs():
         assert bool((big_m == 5.0).all()) and bool((big_o == 5.0).all())
 
 
+# sides of up to 64: all steps in fp32, the last of them, from one step to more than the default
+@pytest.mark.parametrize("coef", [COEF, (1.5, -0.5, 0.0)])
+@pytest.mark.parametrize("steps", [1, 3, 4, 8])
+@pytest.mark.parametrize("rows,cols", [(16, 300), (700, 30), (48, 1000)])
+def test_long_side_steps(rows, cols, steps, coef):
+    rng = _rng(rows, cols, steps, 18)
+    g, t = _store(_gradient(rng, rows, cols, "spiked"), "f32")
+    want, _ = R.orthogonalise(g, None, 0, True, steps, coef, 1e-7, 2.0)
+    _orth_check(ops.orthogonalize(t, steps=steps, coefficients=coef, scale=2.0, dtype=torch.float32), want, "f32")
+
+
 # ---- ... of long matrices with a shorter side of 65 to 128: bands of 128 of the long side, a launch a step ----------------------
 @pytest.mark.parametrize("kind", ["noise", "spiked", "rank"])
 @pytest.mark.parametrize("rows,cols", [(65, 257), (128, 512), (100, 513), (96, 1000), (1001, 127), (700, 66), (128, 4096), (3000, 77)])
