@@ -8,8 +8,8 @@
 // last steps, behind which there is little left to grow (three of five: the steps of 64 x 400 57 -> 41 us).  Three
 // launches: sums of U U^T over ranges of the long side (with the momentum), the steps in one workgroup a matrix, Q X.
 // Bound by: the matrix instructions of one compute unit for one matrix, memory for long ones.
-// Measured (whole call, fp32 with momentum): 16 x 8192 21 us, 32 x 4000 24, 64 x 400 55, 64 x 8192 70 (48 of them the steps), 100 of
-// 64 x 1024 93; by the tiles of the larger ones 99 (16 x 8192), 98 (32 x 4000), 102 (64 x 8192) and 145, with an error of 2.3e-3 to 3.0e-3
+// Measured (whole call, fp32 with momentum): 16 x 8192 18 us, 32 x 4000 25, 64 x 400 55, 64 x 8192 72 (50 of them the steps), 100 of
+// 64 x 1024 92; by the tiles of the larger ones 99 (16 x 8192), 98 (32 x 4000), 102 (64 x 8192) and 145, with an error of 2.3e-3 to 3.0e-3
 // where these have the output's rounding, 1.65e-3 (in an fp32 output 6e-7 to 3e-6).
 #include "ops_internal.h"
 #include "ops_device.h"
@@ -355,10 +355,14 @@ hipError_t narrow(const OrthPrepArgs& a, void* out, float* q, int doubles, bool 
 
 }  // namespace
 
-// up to 32 ranges of the long side for one matrix (their sums are read by one workgroup), fewer for many
+// Ranges of the long side: a workgroup takes 3.5 us a tile, and the workgroup of the steps 0.28 us a range to add them up, so that
+// sqrt(12.5 tiles) of them take least (64 x 65536 120 us instead of 161 with 32 of them, 16 x 65536 30
+// instead of 44); a workgroup a compute unit in all
 int orth_narrow_parts(int l, int batch) {
-  const int tiles = (l + LT - 1) / LT, most = batch >= 256 ? 1 : batch >= 8 ? 256 / batch : 32;
-  return tiles < most ? tiles : most;
+  const int tiles = (l + LT - 1) / LT, most = batch >= 256 ? 1 : 256 / batch;
+  int parts = 1;
+  while (parts < most && parts < tiles && (int64_t)parts * parts < 25 * (int64_t)tiles / 2) ++parts;
+  return parts;
 }
 size_t orth_narrow_part_bytes(int s, int nparts, int batch) { return (size_t)batch * nparts * block_doubles(side(s)) * sizeof(double); }
 size_t orth_narrow_q_bytes(int s, int batch) { return (size_t)batch * (side(s) * side(s) + 4) * sizeof(float); }
